@@ -477,6 +477,104 @@ int wf_synthesis(wf_xform_t plan, const float *y_hat, float *image, hipStream_t 
 /* Release a transform plan.  NULL is ignored. */
 void wf_xform_destroy(wf_xform_t plan);
 
+/*
+ * A key/value cache held in 4 bits, and the attention over it: what an
+ * attention context model needs in place of the masked convolution.  It
+ * decodes in the same wavefront order (Sec. III-A, Eq. 4): a step's latents
+ * join the cache once they are decoded, and the next step's queries attend to
+ * the cached ones, a prefix of the cache when tokens are kept in step order.
+ *
+ * Format: a block of 32 consecutive channels of one token's head (the last
+ * block of a head may be shorter) holds 4-bit values {0, 1/2, 1, 3/2, 2, 3, 4,
+ * 6} with a sign, times 2^e: e is the least integer in [-125, 125] with
+ * 6 * 2^e >= the block's largest magnitude, and x / 2^e is rounded to the
+ * nearest value, a tie to the even code (magnitudes beyond 6 * 2^125 are held
+ * as that).  A block with a value that is not finite reads back as NaN.  4.25
+ * bits a value; the bytes' order in a page is the library's own.
+ *
+ * Tokens lie in pages: token t of sequence b is in page
+ * table[b][t / page] of the pool, at place t % page.
+ */
+typedef struct {
+    int32_t heads;          /* key heads (at most 4096)                                 */
+    int32_t dim;            /* channels of a head: a multiple of 8 in [8, 256]; 64, 128
+                               and 256 use their bytes best (others are padded to them) */
+    int32_t pages;          /* pages of the pool                                        */
+    int32_t page;           /* tokens of a page: a power of two in [32, 1024]           */
+} wf_cache_desc;
+
+typedef struct wf_cache_s *wf_cache_t;
+
+/* [sequence][token][head][dim] DEVICE rows, fp32 or bf16 as the call's
+ * precision says: strides in elements, the channels contiguous, any alignment
+ * that the element allows. */
+typedef struct {
+    void *data;
+    int64_t stride[3];      /* sequence, token, head */
+} wf_rows;
+
+/* Build a cache: the pool (zeros: a token that was never written reads as 0)
+ * and the workspace of its attention calls (64 Ki rows of dim + 2 floats).
+ * Synchronous; uses the current HIP device, on which all its calls run.
+ * Errors: WF_E_INVALID, WF_E_UNSUPPORTED, WF_E_NOMEM, WF_E_HIP. */
+int wf_cache_plan(const wf_cache_desc *desc, wf_cache_t *out);
+
+/*
+ * Quantise tokens into the cache: token i < counts[b] of sequence b is written
+ * at position first[b] + i.  counts == NULL: all n of every sequence.
+ *   k, v    [B][n][heads][dim]
+ *   table   [B][table_pages] DEVICE int32 page numbers
+ *   first   [B], counts [B] DEVICE int32
+ * A token past the table, or in a page outside the pool, is not written, and
+ * the next wf_cache_sync returns WF_E_CAPACITY or WF_E_INVALID.  Two tokens of
+ * one call at one place are a race.  Asynchronous on `stream`.
+ */
+int wf_cache_write(wf_cache_t cache, int32_t precision, const wf_rows *k, const wf_rows *v, int32_t B, int32_t n,
+                   const int32_t *table, int32_t table_pages, const int32_t *first, const int32_t *counts,
+                   hipStream_t stream);
+
+/*
+ * Read tokens back as the values they stand for (exact in either precision):
+ * the arguments of wf_cache_write, with k and v written.  Tokens past
+ * counts[b], past the table or in a page outside the pool are zeros (the
+ * latter two are reported by wf_cache_sync).  Asynchronous on `stream`.
+ */
+int wf_cache_read(wf_cache_t cache, int32_t precision, const wf_rows *k, const wf_rows *v, int32_t B, int32_t n,
+                  const int32_t *table, int32_t table_pages, const int32_t *first, const int32_t *counts,
+                  hipStream_t stream);
+
+/*
+ * Attention over the cache: for every sequence b, query row i and head h,
+ *   out = sum_j softmax_j(scale * q . k_j) v_j
+ * over the tokens j < visible[b][i] (of head h / (q_heads / heads)) whose mask
+ * byte is not 0; zeros where there is none.  Tokens that a row does not see
+ * have no part in it, whatever they hold.
+ *   q, out       [B][n][q_heads][dim], q_heads a multiple of the cache's heads
+ *   visible      [B][n] DEVICE int32: a prefix for each row (the same for all
+ *                rows of a wavefront step, one more for each next row of a
+ *                causal chunk, 0 for a row that is not in use)
+ *   mask         NULL, or DEVICE bytes: mask[b * mask_stride[0] + i *
+ *                mask_stride[1] + j], j < max_visible (mask_stride is HOST)
+ *   max_visible  no row sees more (it sizes the launch); a row that does is
+ *                cut there, and the next wf_cache_sync returns WF_E_CAPACITY
+ *   scale        positive; 1 / sqrt(dim) as a rule
+ * Tokens in a page outside the pool are left out, and the next wf_cache_sync
+ * returns WF_E_INVALID.  Sums are held in fp32, and their order depends on the
+ * call's sizes alone.  Asynchronous on `stream`; one call in flight per cache
+ * (the workspace is shared by its calls).
+ */
+int wf_cache_attend(wf_cache_t cache, int32_t precision, const wf_rows *q, const wf_rows *out, int32_t B, int32_t n,
+                    int32_t q_heads, const int32_t *table, int32_t table_pages, const int32_t *visible,
+                    const uint8_t *mask, const int64_t *mask_stride, int32_t max_visible, float scale,
+                    hipStream_t stream);
+
+/* Wait for `stream` and report an error that the cache's kernels recorded
+ * (see the calls above).  Clears it. */
+int wf_cache_sync(wf_cache_t cache, hipStream_t stream);
+
+/* Release a cache.  NULL is ignored. */
+void wf_cache_destroy(wf_cache_t cache);
+
 /* Release everything the plan owns.  NULL is ignored. */
 void wf_plan_destroy(wf_plan_t plan);
 

@@ -1,0 +1,482 @@
+// Attention over the 4-bit key/value cache:
+//   o_i = sum_j p_ij v_j / sum_j p_ij,   p_ij = exp(scale q_i . k_j - m_i)
+// over the tokens j that row i sees (j < visible_i, and its mask), zeros where
+// it sees none.  One pass over the cache with a running maximum m and sum.
+//
+// Rows are (query, head of the group) pairs that share a key head, 16 to an
+// MFMA column tile.  A wave takes tiles of 32 tokens: S = K Q^T (rows are
+// tokens, columns queries) in two 16 x 16 products, and O^T += V^T P^T (rows
+// are channels).  The operand row r of the first products is the token
+// 8 (r / 4) + r % 4 (+ 4 for the second), so that lane 16 g + c ends up with
+// the scores of query c and tokens 8 g .. 8 g + 7, which is the operand that
+// the second product takes: probabilities stay in their registers.  Keys and
+// values go from memory to registers and become bf16 there, exactly, with the
+// power of their block (one conversion for two values).
+//
+// Operands: keys and values are exact in bf16.  bf16 queries are too; fp32
+// queries are three bf16 parts (24 bits).  Probabilities are two bf16 parts
+// (16 bits) for bf16 calls, so that the output's own rounding is the only one
+// that shows, and three (24 bits) for fp32 calls.  Scores, maxima, sums and
+// outputs are held in fp32; a row's sum is that of its rounded probabilities.
+//
+// The four waves of a workgroup share the tokens and join at the end; with
+// few rows the tokens are also split over workgroups, and a second kernel
+// joins their results.
+#include <cmath>
+
+#include "wf_cache.h"
+
+namespace wf {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
+typedef unsigned u2 __attribute__((ext_vector_type(2)));
+
+constexpr int kAtWaves = 4;
+constexpr int kAtThreads = 64 * kAtWaves;
+// a row's maximum is raised only when a score passes it by this much (in
+// powers of two): its probabilities then stay below 2^8
+constexpr float kAtSlack = 8.0f;
+
+template <class T>
+struct AtParts;
+template <>
+struct AtParts<__bf16> {
+    static constexpr int kQ = 1, kP = 2;
+};
+template <>
+struct AtParts<float> {
+    static constexpr int kQ = 3, kP = 3;
+};
+
+__device__ __forceinline__ f4 mfma(b8 a, b8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// Eight values as N bf16 parts, the largest first.
+template <int N>
+__device__ __forceinline__ void parts(const float (&x)[8], b8 (&p)[N]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float r = x[e];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const __bf16 h = (__bf16)r;
+            p[n][e] = h;
+            r -= (float)h;
+        }
+    }
+}
+
+// Two 4-bit values of byte J of w, times the power, as a pair of bf16.
+template <int J>
+__device__ __forceinline__ unsigned pair_of(unsigned w, float power) {
+    return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, J));
+}
+
+__device__ __forceinline__ b8 key_frag(unsigned w, float power) {
+    u4 r = {pair_of<0>(w, power), pair_of<1>(w, power), pair_of<2>(w, power), pair_of<3>(w, power)};
+    return __builtin_bit_cast(b8, r);
+}
+
+__device__ __forceinline__ float power_of(unsigned byte) { return __builtin_bit_cast(float, byte << 23); }
+
+// A tile of 32 tokens of one head as a lane holds it.
+template <int DP>
+struct AtTile {
+    static constexpr int kKw = DP / 32;          // words of a lane's quarter of a key
+    static constexpr int kVw = DP / 16;          // words of a lane's run of values
+    unsigned k[2][kKw];
+    unsigned kp[2][DP == 256 ? 2 : 1];
+    unsigned v[kVw];
+    unsigned vp[2];
+};
+
+template <int DP>
+__device__ __forceinline__ void load_tile(AtTile<DP>& t, const uint8_t* base, int shift, int token, int lane) {
+    using L = KvLayout<DP>;
+    const int g = lane >> 4, i = lane & 15;
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+        const int key = token + 8 * (i >> 2) + 4 * a + (i & 3);
+        __builtin_memcpy(t.k[a], __builtin_assume_aligned(base + L::k_codes(key) + g * (DP / 8), DP / 8), DP / 8);
+        const uint8_t* p = base + L::k_powers(shift, key) + g * (DP / 4) / kKvBlock;
+        t.kp[a][0] = p[0];
+        if constexpr (DP == 256) t.kp[a][1] = p[1];
+    }
+    const int tile = token / kKvTile;
+    __builtin_memcpy(t.v, __builtin_assume_aligned(base + L::v_codes(shift, tile, g, i), 16), DP / 4);
+    __builtin_memcpy(t.vp, __builtin_assume_aligned(base + L::v_powers(shift, tile, i * L::kRows / kKvBlock) + 8 * g, 8), 8);
+}
+
+// Tiles 2 B and 2 B + 1 of the values as operands: rows are channels kRows i +
+// 2 B (+ 1), k the lane's eight tokens.
+template <int DP, int B>
+__device__ __forceinline__ void value_frags(const unsigned (&v)[DP / 16], const float (&power)[8], b8 (&f)[2]) {
+    u4 lo, hi;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        unsigned x, y;
+        if constexpr (DP == 64) {                 // a word holds two tokens
+            x = pair_of<B>(v[p], power[2 * p]);
+            y = pair_of<B + 2>(v[p], power[2 * p + 1]);
+        } else if constexpr (DP == 128) {
+            x = pair_of<B>(v[2 * p], power[2 * p]);
+            y = pair_of<B>(v[2 * p + 1], power[2 * p + 1]);
+        } else {                                  // two words a token
+            x = pair_of<B % 4>(v[4 * p + B / 4], power[2 * p]);
+            y = pair_of<B % 4>(v[4 * p + 2 + B / 4], power[2 * p + 1]);
+        }
+        lo[p] = __builtin_amdgcn_perm(y, x, 0x05040100);
+        hi[p] = __builtin_amdgcn_perm(y, x, 0x07060302);
+    }
+    f[0] = __builtin_bit_cast(b8, lo);
+    f[1] = __builtin_bit_cast(b8, hi);
+}
+
+template <int DP, int NT, int NP, int B = 0>
+__device__ __forceinline__ void add_values(const unsigned (&v)[DP / 16], const float (&power)[8], const b8 (&p)[NT][NP],
+                                           f4 (&o)[NT][DP / 16]) {
+    if constexpr (B < DP / 32) {
+        b8 f[2];
+        value_frags<DP, B>(v, power, f);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int m = NP - 1; m >= 0; --m)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) o[t][2 * B + s] = mfma(f[s], p[t][m], o[t][2 * B + s]);
+        add_values<DP, NT, NP, B + 1>(v, power, p, o);
+    }
+}
+
+// One workgroup: 16 NT rows of a sequence's key head, and a share of its
+// tokens.
+template <int DP, class T, int NT, bool MASK>
+__global__ __launch_bounds__(kAtThreads) void k_attend(AttendArgs a) {
+    constexpr int NQ = AtParts<T>::kQ, NP = AtParts<T>::kP, NK = DP / 32, ND = DP / 16;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
+    const int rows = a.n * a.group, nrt = (rows + 16 * NT - 1) / (16 * NT);
+    int id = blockIdx.x;
+    const int split = id % a.splits; id /= a.splits;
+    const int rt = nrt - 1 - id % nrt; id /= nrt;      // under a causal order the last rows see most: first
+    const int head = id % a.c.heads, b = id / a.c.heads;
+
+    // the lane's rows: their queries, and how many tokens they see
+    b8 q[NT][NK][NQ];
+    int see[NT], most = 0, least = a.max_visible;
+    const uint8_t* mask[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int row = rt * 16 * NT + t * 16 + col;
+        const bool on = row < rows;
+        const int i = on ? row / a.group : 0, h = head * a.group + (on ? row % a.group : 0);
+        int s = on ? a.visible[(size_t)b * a.n + i] : 0;
+        if (s > a.max_visible) {
+            atomicOr(a.c.err, kErrKvRange);
+            s = a.max_visible;
+        }
+        see[t] = max(s, 0);
+        most = max(most, see[t]);
+        if (on) least = min(least, see[t]);
+        mask[t] = MASK ? a.mask + b * a.mb + i * a.mr : nullptr;
+        const T* p = (const T*)a.q.p + b * a.q.sb + i * a.q.sr + h * a.q.sh;
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk) {
+            const int d = DP / 4 * g + 8 * kk;
+            float x[8];
+            if (on && d + 8 <= a.c.dim) {
+                T r[8];
+                __builtin_memcpy(r, p + d, sizeof r);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = (float)r[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = 0.0f;
+            }
+            parts<NQ>(x, q[t][kk]);
+        }
+    }
+#pragma unroll
+    for (int x = 1; x < 16; x <<= 1) {
+        most = max(most, __shfl_xor(most, x));
+        least = min(least, __shfl_xor(least, x));
+    }
+    most = __builtin_amdgcn_readfirstlane(most);
+    least = __builtin_amdgcn_readfirstlane(least);
+
+    // the tiles of this split, dealt to the waves in turn
+    const int tiles = (most + kKvTile - 1) / kKvTile;
+    const int share = (tiles + a.splits - 1) / a.splits;
+    const int t0 = split * share, t1 = min(tiles, t0 + share);
+    const int* table = a.table + (size_t)b * a.table_pages;
+    const int in_page = a.c.page_shift - 5;
+    const size_t head_at = (size_t)head * a.c.head_bytes(), page_bytes = a.c.page_bytes();
+
+    f4 o[NT][ND], l[NT], bad[NT];
+    float m[NT], sub[NT];
+    b8 ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.0f;
+
+    // The pass is repeated with care where a value that is not a number
+    // reached an output: it may stand at a token that only other rows see, and
+    // 0 times it is not 0.  With care such blocks are taken as zeros, and a
+    // count of those that each row sees says which channels they spoil.
+    for (int care = 0; care < 2; ++care) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int r = 0; r < ND; ++r) o[t][r] = f4{0, 0, 0, 0};
+            l[t] = bad[t] = f4{0, 0, 0, 0};
+            m[t] = -INFINITY;
+            sub[t] = 0.0f;
+        }
+        for (int tile = t0 + wave; tile < t1; tile += kAtWaves) {
+            int page = table[tile >> in_page];
+            const bool there = page >= 0 && page < a.c.pages;
+            if (!there) {
+                if (lane == 0) atomicOr(a.c.err, kErrKvPage);
+                continue;
+            }
+            AtTile<DP> x;
+            load_tile<DP>(x, a.c.pool + (size_t)page * page_bytes + head_at, a.c.page_shift,
+                          (tile & ((1 << in_page) - 1)) * kKvTile, lane);
+            f4 s[NT][2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) s[t][h] = f4{0, 0, 0, 0};
+#pragma unroll
+                for (int kk = 0; kk < NK; ++kk) {
+                    const b8 f = key_frag(x.k[h][kk], power_of(x.kp[h][DP == 256 ? kk / 4 : 0]));
+#pragma unroll
+                    for (int n = NQ - 1; n >= 0; --n)
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) s[t][h] = mfma(f, q[t][kk][n], s[t][h]);
+                }
+            }
+            const int at = tile * kKvTile + 8 * g;         // the lane's first token
+            const bool whole = !MASK && (tile + 1) * kKvTile <= least;
+            unsigned char sees[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                sees[t] = 0xff;
+                if (!whole) {
+                    sees[t] = 0;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        bool on = at + e < see[t];
+                        if constexpr (MASK) on = on && mask[t][at + e];
+                        sees[t] |= on << e;
+                        s[t][e / 4][e % 4] = on ? s[t][e / 4][e % 4] : -INFINITY;
+                    }
+                }
+            }
+            float power[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) power[e] = power_of(x.vp[e / 4] >> 8 * (e % 4) & 0xff);
+            if ((tile + 1) * kKvTile > most) {
+                // past the last token that any row sees, a page holds anything
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (at + e >= most) power[e] = 1.0f;
+            }
+            if (care) {
+                unsigned spoilt = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (power[e] == INFINITY) {
+                        spoilt |= 1u << e;
+                        power[e] = 1.0f;
+                    }
+                b8 is;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) is[e] = (__bf16)(float)(spoilt >> e & 1);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    b8 on;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) on[e] = (__bf16)(float)(sees[t] >> e & 1);
+                    bad[t] = mfma(is, on, bad[t]);
+                }
+            }
+            b8 p[NT][NP];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                float top = s[t][0][0];
+#pragma unroll
+                for (int e = 1; e < 8; ++e) top = fmaxf(top, s[t][e / 4][e % 4]);
+                top *= a.scale_log2;
+                if (__any(top > (m[t] == -INFINITY ? -INFINITY : m[t] + kAtSlack))) {
+                    top = fmaxf(top, __shfl_xor(top, 16));
+                    top = fmaxf(top, __shfl_xor(top, 32));
+                    const float next = fmaxf(m[t], top), by = m[t] == -INFINITY ? 0.0f : exp2f(m[t] - next);
+                    if (next != -INFINITY) {
+                        m[t] = sub[t] = next;
+#pragma unroll
+                        for (int r = 0; r < ND; ++r) o[t][r] *= by;
+                        l[t] *= by;
+                    }
+                }
+                float w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e / 4][e % 4], a.scale_log2, -sub[t]));
+                parts<NP>(w, p[t]);
+#pragma unroll
+                for (int n = NP - 1; n >= 0; --n) l[t] = mfma(ones, p[t][n], l[t]);
+            }
+            add_values<DP, NT, NP>(x.v, power, p, o);
+        }
+        if (care) break;
+        bool nan = false;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int r = 0; r < ND; ++r)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) nan |= o[t][r][e] != o[t][r][e];
+        if (!__any(nan)) break;
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (bad[t][e] > 0.0f)
+#pragma unroll
+                for (int r = 0; r < ND; ++r) o[t][r][e] = __builtin_nanf("");
+
+    // join the waves, one tile of 16 rows after the other
+    constexpr int kPitch = DP + 4;
+    __shared__ float so[kAtWaves][16 * kPitch];
+    __shared__ float sm[kAtWaves][16], sl[kAtWaves][16];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        __syncthreads();
+        if (lane < 16) {
+            sm[wave][lane] = m[t];
+            sl[wave][lane] = l[t][0];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int r = 0; r < ND; r += 4)
+                *(f4*)&so[wave][col * kPitch + ND * (4 * g + e) + r] = f4{o[t][r][e], o[t][r + 1][e], o[t][r + 2][e], o[t][r + 3][e]};
+        __syncthreads();
+        for (int x = threadIdx.x; x < 16 * DP / 8; x += kAtThreads) {
+            const int c = x / (DP / 8), d = x % (DP / 8) * 8, row = rt * 16 * NT + t * 16 + c;
+            if (row >= rows) continue;
+            float top = sm[0][c], sum = 0.0f, v[8] = {};
+#pragma unroll
+            for (int w = 1; w < kAtWaves; ++w) top = fmaxf(top, sm[w][c]);
+#pragma unroll
+            for (int w = 0; w < kAtWaves; ++w) {
+                if (sm[w][c] == -INFINITY && sl[w][c] == 0.0f) continue;      // it saw no token
+                const float by = sm[w][c] == top ? 1.0f : exp2f(sm[w][c] - top);
+                sum += by * sl[w][c];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += by * so[w][c * kPitch + d + e];
+            }
+            const int i = row / a.group, h = head * a.group + row % a.group;
+            if (a.splits == 1) {
+                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                if (d < a.c.dim) {
+                    T out[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) out[e] = (T)(v[e] * inv);
+                    __builtin_memcpy((T*)a.o.p + b * a.o.sb + i * a.o.sr + h * a.o.sh + d, out, sizeof out);
+                }
+            } else {
+                const size_t at = (((size_t)b * a.n + i) * (a.c.heads * a.group) + h) * a.splits + split;
+                __builtin_memcpy(a.part_o + at * DP + d, v, sizeof v);
+                if (d == 0) {
+                    a.part_ml[at * 2] = top;
+                    a.part_ml[at * 2 + 1] = sum;
+                }
+            }
+        }
+    }
+}
+
+// Joins the splits of a row: eight channels a lane.
+template <int DP, class T>
+__global__ __launch_bounds__(kAtThreads) void k_attend_join(AttendArgs a) {
+    constexpr int W = DP / 8;
+    const long long id = (long long)blockIdx.x * kAtThreads + threadIdx.x, row = id / W;
+    const int d = id % W * 8, hq = a.c.heads * a.group;
+    if (row >= (long long)a.B * a.n * hq || d >= a.c.dim) return;
+    const float* ml = a.part_ml + row * a.splits * 2;
+    const float* po = a.part_o + row * a.splits * DP + d;
+    float top = -INFINITY, sum = 0.0f, v[8] = {};
+    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[2 * s]);
+    for (int s = 0; s < a.splits; ++s) {
+        const float m = ml[2 * s], l = ml[2 * s + 1];
+        if (m == -INFINITY && l == 0.0f) continue;
+        const float by = m == top ? 1.0f : exp2f(m - top);
+        sum += by * l;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += by * po[(size_t)s * DP + e];
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const int h = row % hq;
+    const long long bi = row / hq;
+    T out[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) out[e] = (T)(v[e] * inv);
+    __builtin_memcpy((T*)a.o.p + bi / a.n * a.o.sb + bi % a.n * a.o.sr + h * a.o.sh + d, out, sizeof out);
+}
+
+// ---- host -----------------------------------------------------------------------
+
+// Column tiles of a workgroup.
+static int row_tiles(const AttendArgs& a, int precision) {
+    const int rows = a.n * a.group, most = precision == WF_FP32 ? (a.c.dp == 256 ? 1 : 2) : (a.c.dp == 256 ? 2 : 4);
+    return rows <= 16 || most == 1 ? 1 : (rows <= 32 || most == 2 ? 2 : 4);
+}
+
+long long attend_plan(AttendArgs& a, int precision) {
+    const int nt = row_tiles(a, precision), rows = a.n * a.group;
+    const long long groups = (long long)a.B * a.c.heads * ((rows + 16 * nt - 1) / (16 * nt));
+    const long long all = (long long)a.B * a.n * a.c.heads * a.group;
+    // workgroups that keep the chip busy, with at least two tiles for each wave
+    long long s = (1024 + groups - 1) / groups;
+    const long long by_len = a.max_visible / (2 * kAtWaves * kKvTile);
+    s = s < by_len ? s : by_len;
+    const long long by_room = kAttendWorkRows / all;
+    s = s < by_room ? s : by_room;
+    a.splits = s < 2 ? 1 : (int)s;
+    return a.splits == 1 ? 0 : all * a.splits;
+}
+
+template <int DP, class T, int NT>
+static void launch_nt(const AttendArgs& a, hipStream_t st) {
+    const int rows = a.n * a.group;
+    const long long groups = (long long)a.B * a.c.heads * ((rows + 16 * NT - 1) / (16 * NT));
+    const dim3 grid((unsigned)(groups * a.splits));
+    if (a.mask) hipLaunchKernelGGL((k_attend<DP, T, NT, true>), grid, dim3(kAtThreads), 0, st, a);
+    else hipLaunchKernelGGL((k_attend<DP, T, NT, false>), grid, dim3(kAtThreads), 0, st, a);
+    if (a.splits > 1) {
+        const long long lanes = (long long)a.B * a.n * a.c.heads * a.group * (DP / 8);
+        hipLaunchKernelGGL((k_attend_join<DP, T>), dim3((unsigned)((lanes + kAtThreads - 1) / kAtThreads)), dim3(kAtThreads), 0, st, a);
+    }
+}
+
+template <int DP>
+static void launch_dp(const AttendArgs& a, int precision, hipStream_t st) {
+    const int nt = row_tiles(a, precision);
+    if (precision == WF_BF16) {
+        if (nt == 1) launch_nt<DP, __bf16, 1>(a, st);
+        else if (nt == 2) launch_nt<DP, __bf16, 2>(a, st);
+        else if constexpr (DP < 256) launch_nt<DP, __bf16, 4>(a, st);
+    } else {
+        if (nt == 1) launch_nt<DP, float, 1>(a, st);
+        else if constexpr (DP < 256) launch_nt<DP, float, 2>(a, st);
+    }
+}
+
+void launch_attend(const AttendArgs& a, int precision, hipStream_t st) {
+    if (a.c.dp == 64) launch_dp<64>(a, precision, st);
+    else if (a.c.dp == 128) launch_dp<128>(a, precision, st);
+    else launch_dp<256>(a, precision, st);
+}
+
+}  // namespace wf

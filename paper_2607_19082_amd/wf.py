@@ -24,7 +24,8 @@ DRIVER = {"stream": 0, "graph": 1, "persistent": 2, "dataflow": 3, "resident": 4
 EXPORTS = ["wf_schedule", "wf_validate", "wf_plan", "wf_plan_schedule", "wf_plan_deps", "wf_plan_set_waits", "wf_litmus", "wf_decode",
            "wf_encode", "wf_ec_tables", "wf_mix_tables", "wf_encode_bits", "wf_decode_bits", "wf_plan_trace",
            "wf_measure_floor", "wf_plan_sync", "wf_xform_plan", "wf_hyper_synthesis", "wf_synthesis",
-           "wf_decode_noalloc", "wf_xform_destroy", "wf_plan_destroy", "wf_last_error"]
+           "wf_decode_noalloc", "wf_cache_plan", "wf_cache_write", "wf_cache_read", "wf_cache_attend", "wf_cache_sync",
+           "wf_cache_destroy", "wf_xform_destroy", "wf_plan_destroy", "wf_last_error"]
 
 
 class WfError(RuntimeError):
@@ -58,6 +59,15 @@ class XformDesc(ctypes.Structure):
         ("gs_w", ctypes.c_void_p * 4), ("gs_b", ctypes.c_void_p * 4),
         ("gdn_beta", ctypes.c_void_p * 3), ("gdn_gamma", ctypes.c_void_p * 3),
     ]
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = [("heads", ctypes.c_int32), ("dim", ctypes.c_int32), ("pages", ctypes.c_int32),
+                ("page", ctypes.c_int32)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_int64 * 3)]
 
 
 class Out(ctypes.Structure):
@@ -96,6 +106,14 @@ def lib():
         L.wf_hyper_synthesis.argtypes = [P, P, P, P]
         L.wf_synthesis.argtypes = [P, P, P, P]
         L.wf_xform_destroy.argtypes = [P]
+        i32 = ctypes.c_int32
+        rows = ctypes.POINTER(Rows)
+        L.wf_cache_plan.argtypes = [ctypes.POINTER(CacheDesc), ctypes.POINTER(ctypes.c_void_p)]
+        L.wf_cache_write.argtypes = [P, i32, rows, rows, i32, i32, P, i32, P, P, P]
+        L.wf_cache_read.argtypes = [P, i32, rows, rows, i32, i32, P, i32, P, P, P]
+        L.wf_cache_attend.argtypes = [P, i32, rows, rows, i32, i32, i32, P, i32, P, P, P, i32, ctypes.c_float, P]
+        L.wf_cache_sync.argtypes = [P, P]
+        L.wf_cache_destroy.argtypes = [P]
         L.wf_plan_trace.argtypes = [P, P, ctypes.c_int64, P, P]
         L.wf_measure_floor.argtypes = [P, P, P]
         L.wf_plan_sync.argtypes = [P, P]
@@ -105,6 +123,7 @@ def lib():
         for name in EXPORTS[:-2]:
             getattr(L, name).restype = ctypes.c_int
         L.wf_xform_destroy.restype = None
+        L.wf_cache_destroy.restype = None
         _lib = L
     return _lib
 
@@ -432,3 +451,133 @@ class Xform:
         _check(lib().wf_synthesis(self._h, self._ptr(y_hat, (B, H, W, M), "y_hat"),
                                   self._ptr(image, (B, 16 * H, 16 * W, 3), "image"), _stream_handle(stream)))
         return image
+
+
+class Cache:
+    """A key/value cache held in 4 bits, in pages, and the attention over it
+    (wf_cache_*; the format is described there).
+
+    heads, dim   key heads and channels of a head (a multiple of 8, up to 256)
+    pages, page  pages of the pool, tokens of a page (a power of two, 32 to 1024)
+
+    Token t of sequence b lies in page table[b, t // page].  Tensors are torch
+    tensors on the current HIP device, fp32 or bf16 where they hold channels
+    (contiguous; sequence, token and head may have any strides) and contiguous
+    int32 elsewhere.  Calls are asynchronous on the given (default: current)
+    torch stream; one attend call in flight per cache.  sync() waits and raises
+    what a kernel found wrong."""
+
+    def __init__(self, heads, dim, pages, page=64):
+        h = ctypes.c_void_p()
+        _check(lib().wf_cache_plan(ctypes.byref(CacheDesc(heads, dim, pages, page)), ctypes.byref(h)))
+        self._h = h
+        self.heads, self.dim, self.pages, self.page = heads, dim, pages, page
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib().wf_cache_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    @staticmethod
+    def _rows(t, shape, dtype, name):
+        if not t.is_cuda or t.dtype != dtype or t.shape != shape or (t.stride(3) != 1 and t.numel()):
+            raise ValueError(f"{name}: expected a {dtype} CUDA tensor {tuple(shape)} with contiguous channels, got "
+                             f"{t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
+        st = t.stride()
+        return Rows(t.data_ptr(), (st[0], st[1], st[2]))
+
+    @staticmethod
+    def _ints(t, shape, name):
+        import torch
+        if not t.is_cuda or t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name}: expected a contiguous int32 CUDA tensor {tuple(shape)}, got {t.dtype} "
+                             f"{tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    @staticmethod
+    def _precision(dtype):
+        import torch
+        if dtype == torch.bfloat16:
+            return 1
+        if dtype == torch.float32:
+            return 0
+        raise ValueError(f"expected torch.float32 or torch.bfloat16, got {dtype}")
+
+    def _tokens(self, B, n, table, first, counts):
+        if table.dim() != 2:
+            raise ValueError(f"table: expected two dimensions, got {tuple(table.shape)}")
+        pages = table.shape[1]
+        return (self._ints(table, (B, pages), "table"), pages, self._ints(first, (B,), "first"),
+                None if counts is None else self._ints(counts, (B,), "counts"))
+
+    def write(self, k, v, table, first, counts=None, stream=None):
+        """Quantise k and v [B][n][heads][dim] into the cache: token i of
+        sequence b at position first[b] + i, where i < counts[b] (None: all)."""
+        if k.dim() != 4:
+            raise ValueError(f"k: expected four dimensions, got {tuple(k.shape)}")
+        B, n = k.shape[:2]
+        shape = (B, n, self.heads, self.dim)
+        kr, vr = self._rows(k, shape, k.dtype, "k"), self._rows(v, shape, k.dtype, "v")
+        p_table, pages, p_first, p_counts = self._tokens(B, n, table, first, counts)
+        _check(lib().wf_cache_write(self._h, self._precision(k.dtype), kr, vr, B, n, p_table, pages, p_first, p_counts,
+                                    _stream_handle(stream)))
+
+    def read(self, table, first, n, counts=None, dtype=None, out=None, stream=None):
+        """Tokens first[b] .. first[b] + n - 1 of every sequence as the values
+        they stand for: (k, v) [B][n][heads][dim] of `dtype` (default fp32), or
+        written to the pair `out`.  Tokens past counts[b] are zeros."""
+        import torch
+        B = table.shape[0]
+        shape = (B, n, self.heads, self.dim)
+        if out is None:
+            dtype = torch.float32 if dtype is None else dtype
+            out = (torch.empty(shape, dtype=dtype, device=table.device), torch.empty(shape, dtype=dtype, device=table.device))
+        k, v = out
+        kr, vr = self._rows(k, shape, k.dtype, "k"), self._rows(v, shape, k.dtype, "v")
+        p_table, pages, p_first, p_counts = self._tokens(B, n, table, first, counts)
+        _check(lib().wf_cache_read(self._h, self._precision(k.dtype), kr, vr, B, n, p_table, pages, p_first, p_counts,
+                                   _stream_handle(stream)))
+        return k, v
+
+    def attend(self, q, table, visible, scale=None, mask=None, max_visible=None, out=None, stream=None):
+        """Attention of q [B][n][q_heads][dim] over the cached tokens: row i of
+        sequence b sees tokens j < visible[b, i] (int32 [B][n]) and, with a mask
+        (bool [B][n][max_visible], any strides of sequence and row), those that
+        it allows; a row that sees none gives zeros.  q_heads is a multiple of
+        the cache's heads; scale defaults to dim ** -0.5.  max_visible bounds
+        visible (default: the mask's width, or all that the table holds; a
+        tighter bound makes a better launch)."""
+        import torch
+        if q.dim() != 4:
+            raise ValueError(f"q: expected four dimensions, got {tuple(q.shape)}")
+        B, n, hq = q.shape[:3]
+        shape = (B, n, hq, self.dim)
+        if table.dim() != 2:
+            raise ValueError(f"table: expected two dimensions, got {tuple(table.shape)}")
+        pages = table.shape[1]
+        if max_visible is None:
+            max_visible = pages * self.page if mask is None else mask.shape[-1]
+        if out is None:
+            out = torch.empty(shape, dtype=q.dtype, device=q.device)
+        qr, outr = self._rows(q, shape, q.dtype, "q"), self._rows(out, shape, q.dtype, "out")
+        p_mask = strides = None
+        if mask is not None:
+            if not mask.is_cuda or mask.dtype != torch.bool or mask.shape != (B, n, max_visible) or \
+                    (max_visible > 1 and mask.stride(2) != 1):
+                raise ValueError(f"mask: expected a bool CUDA tensor {(B, n, max_visible)} with contiguous tokens, got "
+                                 f"{mask.dtype} {tuple(mask.shape)}, strides {mask.stride()}")
+            p_mask, strides = mask.data_ptr(), (ctypes.c_int64 * 2)(mask.stride(0), mask.stride(1))
+        _check(lib().wf_cache_attend(self._h, self._precision(q.dtype), qr, outr, B, n, hq,
+                                     self._ints(table, (B, pages), "table"), pages, self._ints(visible, (B, n), "visible"),
+                                     p_mask, strides, max_visible, self.dim ** -0.5 if scale is None else scale,
+                                     _stream_handle(stream)))
+        return out
+
+    def sync(self, stream=None):
+        _check(lib().wf_cache_sync(self._h, _stream_handle(stream)))
