@@ -73,39 +73,56 @@ __device__ __forceinline__ unsigned pair_of(unsigned w, float power) {
     return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, J));
 }
 
-__device__ __forceinline__ b8 key_frag(unsigned w, float power) {
+// A tile of 32 tokens of one head as a lane holds it.
+template <int DP>
+struct AtTile {
+    unsigned k[DP / 16], v[DP / 16], kp, vp[2];
+};
+
+template <int DP>
+__device__ __forceinline__ void load_tile(AtTile<DP>& t, const uint8_t* record, int lane) {
+    using L = KvLayout<DP>;
+#pragma unroll
+    for (int n = 0; n < L::kLane; n += 16) {
+        __builtin_memcpy(t.k + n / 4, __builtin_assume_aligned(record + L::piece(lane, n), 16), 16);
+        __builtin_memcpy(t.v + n / 4, __builtin_assume_aligned(record + 16 * DP + L::piece(lane, n), 16), 16);
+    }
+    if constexpr (L::kPowers == 2) {
+        uint16_t p;
+        __builtin_memcpy(&p, __builtin_assume_aligned(record + L::key_lane_powers(lane), 2), 2);
+        t.kp = p;
+    } else {
+        __builtin_memcpy(&t.kp, __builtin_assume_aligned(record + L::key_lane_powers(lane), 4), 4);
+    }
+    __builtin_memcpy(t.vp, __builtin_assume_aligned(record + L::value_powers((lane & 15) * L::kRows / kKvBlock) + 8 * (lane >> 4), 8), 8);
+}
+
+// Byte N of a word as a power of two.
+template <int N>
+__device__ __forceinline__ float power_at(unsigned w) {
+    return __builtin_bit_cast(float, (N == 0 ? w << 23 : (N == 1 ? w << 15 : (N == 2 ? w << 7 : w >> 1))) & 0x7f800000u);
+}
+
+// The operand of half A of the keys, channels from 8 KK of each quarter.
+template <int DP, int A, int KK>
+__device__ __forceinline__ b8 key_frag(const AtTile<DP>& t) {
+    constexpr int kPerLane = KvLayout<DP>::kPowers / 2;    // powers of a half in a lane
+    const unsigned w = t.k[A * (DP / 32) + KK];
+    const float power = power_at<A * kPerLane + KK * kPerLane / (DP / 32)>(t.kp);
     u4 r = {pair_of<0>(w, power), pair_of<1>(w, power), pair_of<2>(w, power), pair_of<3>(w, power)};
     return __builtin_bit_cast(b8, r);
 }
 
-__device__ __forceinline__ float power_of(unsigned byte) { return __builtin_bit_cast(float, byte << 23); }
-
-// A tile of 32 tokens of one head as a lane holds it.
-template <int DP>
-struct AtTile {
-    static constexpr int kKw = DP / 32;          // words of a lane's quarter of a key
-    static constexpr int kVw = DP / 16;          // words of a lane's run of values
-    unsigned k[2][kKw];
-    unsigned kp[2][DP == 256 ? 2 : 1];
-    unsigned v[kVw];
-    unsigned vp[2];
-};
-
-template <int DP>
-__device__ __forceinline__ void load_tile(AtTile<DP>& t, const uint8_t* base, int shift, int token, int lane) {
-    using L = KvLayout<DP>;
-    const int g = lane >> 4, i = lane & 15;
+template <int DP, int NT, int NQ, int A, int KK = 0>
+__device__ __forceinline__ void add_scores(const AtTile<DP>& x, const b8 (&q)[NT][DP / 32][NQ], f4 (&s)[NT][2]) {
+    if constexpr (KK < DP / 32) {
+        const b8 f = key_frag<DP, A, KK>(x);
 #pragma unroll
-    for (int a = 0; a < 2; ++a) {
-        const int key = token + 8 * (i >> 2) + 4 * a + (i & 3);
-        __builtin_memcpy(t.k[a], __builtin_assume_aligned(base + L::k_codes(key) + g * (DP / 8), DP / 8), DP / 8);
-        const uint8_t* p = base + L::k_powers(shift, key) + g * (DP / 4) / kKvBlock;
-        t.kp[a][0] = p[0];
-        if constexpr (DP == 256) t.kp[a][1] = p[1];
+        for (int n = NQ - 1; n >= 0; --n)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) s[t][A] = mfma(f, q[t][KK][n], s[t][A]);
+        add_scores<DP, NT, NQ, A, KK + 1>(x, q, s);
     }
-    const int tile = token / kKvTile;
-    __builtin_memcpy(t.v, __builtin_assume_aligned(base + L::v_codes(shift, tile, g, i), 16), DP / 4);
-    __builtin_memcpy(t.vp, __builtin_assume_aligned(base + L::v_powers(shift, tile, i * L::kRows / kKvBlock) + 8 * g, 8), 8);
 }
 
 // Tiles 2 B and 2 B + 1 of the values as operands: rows are channels kRows i +
@@ -149,12 +166,17 @@ __device__ __forceinline__ void add_values(const unsigned (&v)[DP / 16], const f
     }
 }
 
+// Workgroups of a compute unit that the registers are shared out for.
+template <int DP, class T, int NT>
+constexpr int kAtWgs = NT * DP * (int)sizeof(T) <= 128 * 2 ? 3 : (NT * DP * (int)sizeof(T) <= 256 * 2 ? 2 : 1);
+
 // One workgroup: 16 NT rows of a sequence's key head, and a share of its
 // tokens.
 template <int DP, class T, int NT, bool MASK>
-__global__ __launch_bounds__(kAtThreads) void k_attend(AttendArgs a) {
+__global__ __launch_bounds__(kAtThreads, (kAtWgs<DP, T, NT>)) void k_attend(AttendArgs a) {
     constexpr int NQ = AtParts<T>::kQ, NP = AtParts<T>::kP, NK = DP / 32, ND = DP / 16;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
+    using L = KvLayout<DP>;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int rows = a.n * a.group, nrt = (rows + 16 * NT - 1) / (16 * NT);
     int id = blockIdx.x;
     const int split = id % a.splits; id /= a.splits;
@@ -210,7 +232,8 @@ __global__ __launch_bounds__(kAtThreads) void k_attend(AttendArgs a) {
     const int t0 = split * share, t1 = min(tiles, t0 + share);
     const int* table = a.table + (size_t)b * a.table_pages;
     const int in_page = a.c.page_shift - 5;
-    const size_t head_at = (size_t)head * a.c.head_bytes(), page_bytes = a.c.page_bytes();
+    const uint8_t* pool = a.c.pool + (size_t)head * a.c.head_bytes();
+    const size_t page_bytes = a.c.page_bytes();
 
     f4 o[NT][ND], l[NT], bad[NT];
     float m[NT], sub[NT];
@@ -231,30 +254,19 @@ __global__ __launch_bounds__(kAtThreads) void k_attend(AttendArgs a) {
             m[t] = -INFINITY;
             sub[t] = 0.0f;
         }
-        for (int tile = t0 + wave; tile < t1; tile += kAtWaves) {
-            int page = table[tile >> in_page];
+        AtTile<DP> buf[2];
+        auto load = [&](AtTile<DP>& x, int tile) {
+            const int page = table[tile >> in_page];
             const bool there = page >= 0 && page < a.c.pages;
-            if (!there) {
-                if (lane == 0) atomicOr(a.c.err, kErrKvPage);
-                continue;
-            }
-            AtTile<DP> x;
-            load_tile<DP>(x, a.c.pool + (size_t)page * page_bytes + head_at, a.c.page_shift,
-                          (tile & ((1 << in_page) - 1)) * kKvTile, lane);
+            load_tile<DP>(x, pool + (size_t)(there ? page : 0) * page_bytes + (size_t)(tile & ((1 << in_page) - 1)) * L::kRecord, lane);
+            return there;
+        };
+        auto take = [&](const AtTile<DP>& x, int tile) {
             f4 s[NT][2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int t = 0; t < NT; ++t) s[t][h] = f4{0, 0, 0, 0};
-#pragma unroll
-                for (int kk = 0; kk < NK; ++kk) {
-                    const b8 f = key_frag(x.k[h][kk], power_of(x.kp[h][DP == 256 ? kk / 4 : 0]));
-#pragma unroll
-                    for (int n = NQ - 1; n >= 0; --n)
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) s[t][h] = mfma(f, q[t][kk][n], s[t][h]);
-                }
-            }
+            for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = f4{0, 0, 0, 0};
+            add_scores<DP, NT, NQ, 0>(x, q, s);
+            add_scores<DP, NT, NQ, 1>(x, q, s);
             const int at = tile * kKvTile + 8 * g;         // the lane's first token
             const bool whole = !MASK && (tile + 1) * kKvTile <= least;
             unsigned char sees[NT];
@@ -272,9 +284,8 @@ __global__ __launch_bounds__(kAtThreads) void k_attend(AttendArgs a) {
                     }
                 }
             }
-            float power[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) power[e] = power_of(x.vp[e / 4] >> 8 * (e % 4) & 0xff);
+            float power[8] = {power_at<0>(x.vp[0]), power_at<1>(x.vp[0]), power_at<2>(x.vp[0]), power_at<3>(x.vp[0]),
+                              power_at<0>(x.vp[1]), power_at<1>(x.vp[1]), power_at<2>(x.vp[1]), power_at<3>(x.vp[1])};
             if ((tile + 1) * kKvTile > most) {
                 // past the last token that any row sees, a page holds anything
 #pragma unroll
@@ -326,6 +337,19 @@ __global__ __launch_bounds__(kAtThreads) void k_attend(AttendArgs a) {
                 for (int n = NP - 1; n >= 0; --n) l[t] = mfma(ones, p[t][n], l[t]);
             }
             add_values<DP, NT, NP>(x.v, power, p, o);
+        };
+        // the next tile is loaded while this one is worked on
+        int tile = t0 + wave;
+        bool there[2] = {tile < t1 && load(buf[0], tile), false};
+        while (tile < t1) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (tile >= t1) break;
+                there[1 - h] = tile + kAtWaves < t1 && load(buf[1 - h], tile + kAtWaves);
+                if (there[h]) take(buf[h], tile);
+                else if (lane == 0) atomicOr(a.c.err, kErrKvPage);
+                tile += kAtWaves;
+            }
         }
         if (care) break;
         bool nan = false;
@@ -397,25 +421,38 @@ __global__ __launch_bounds__(kAtThreads) void k_attend(AttendArgs a) {
     }
 }
 
-// Joins the splits of a row: eight channels a lane.
+// Joins the splits of one row: eight channels a lane, the splits dealt to
+// groups of lanes that join at the end.
 template <int DP, class T>
 __global__ __launch_bounds__(kAtThreads) void k_attend_join(AttendArgs a) {
-    constexpr int W = DP / 8;
-    const long long id = (long long)blockIdx.x * kAtThreads + threadIdx.x, row = id / W;
-    const int d = id % W * 8, hq = a.c.heads * a.group;
-    if (row >= (long long)a.B * a.n * hq || d >= a.c.dim) return;
+    constexpr int W = DP / 8, G = kAtThreads / W;
+    __shared__ float so[G][DP], sm[G], sl[G];
+    const long long row = blockIdx.x;
+    const int d = threadIdx.x % W * 8, g = threadIdx.x / W, hq = a.c.heads * a.group;
     const float* ml = a.part_ml + row * a.splits * 2;
     const float* po = a.part_o + row * a.splits * DP + d;
     float top = -INFINITY, sum = 0.0f, v[8] = {};
-    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[2 * s]);
-    for (int s = 0; s < a.splits; ++s) {
-        const float m = ml[2 * s], l = ml[2 * s + 1];
-        if (m == -INFINITY && l == 0.0f) continue;
-        const float by = m == top ? 1.0f : exp2f(m - top);
-        sum += by * l;
+    auto add = [&](float m, float l, const float* x) {
+        if (m == -INFINITY && l == 0.0f) return;         // it saw no token
+        const float next = fmaxf(top, m), old = top == next ? 1.0f : exp2f(top - next), by = m == next ? 1.0f : exp2f(m - next);
+        sum = old * sum + by * l;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += by * po[(size_t)s * DP + e];
+        for (int e = 0; e < 8; ++e) v[e] = old * v[e] + by * x[e];
+        top = next;
+    };
+    for (int s = g; s < a.splits; s += G) {
+        float x[8];
+        __builtin_memcpy(x, __builtin_assume_aligned(po + (size_t)s * DP, 16), sizeof x);
+        add(ml[2 * s], ml[2 * s + 1], x);
     }
+    __builtin_memcpy(&so[g][d], v, sizeof v);
+    if (d == 0) {
+        sm[g] = top;
+        sl[g] = sum;
+    }
+    __syncthreads();
+    if (g || d >= a.c.dim) return;
+    for (int j = 1; j < G; ++j) add(sm[j], sl[j], &so[j][d]);
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     const int h = row % hq;
     const long long bi = row / hq;
@@ -455,8 +492,8 @@ static void launch_nt(const AttendArgs& a, hipStream_t st) {
     if (a.mask) hipLaunchKernelGGL((k_attend<DP, T, NT, true>), grid, dim3(kAtThreads), 0, st, a);
     else hipLaunchKernelGGL((k_attend<DP, T, NT, false>), grid, dim3(kAtThreads), 0, st, a);
     if (a.splits > 1) {
-        const long long lanes = (long long)a.B * a.n * a.c.heads * a.group * (DP / 8);
-        hipLaunchKernelGGL((k_attend_join<DP, T>), dim3((unsigned)((lanes + kAtThreads - 1) / kAtThreads)), dim3(kAtThreads), 0, st, a);
+        const long long all = (long long)a.B * a.n * a.c.heads * a.group;
+        hipLaunchKernelGGL((k_attend_join<DP, T>), dim3((unsigned)all), dim3(kAtThreads), 0, st, a);
     }
 }
 

@@ -7,21 +7,25 @@
 // converts two of these values with their power in one instruction, so the
 // matrix operands come from the cache's words without a table.
 //
-// A page holds `page` tokens of every head, head by head, so that a wave
-// streams one head's keys and values as long runs.  Of one head, with DP the
-// head size rounded up to 64, 128 or 256 and P the page's tokens:
-//   key values    [P][DP/2] bytes, channel d in the low (even d) or high half
-//                 of byte d/2: an MFMA operand row is a key, and each of its
-//                 four k-groups of lanes reads a quarter of the head in one run
-//   key powers    [P][DP/32]
-//   value values  [P/32][4][16][8][DP/32] bytes: of a group of 32 tokens,
-//                 eight tokens of DP/16 channels together for each lane of the
-//                 operand whose rows are channels and whose k axis is tokens
-//                 (lane 16 g + i: tokens 8 g .. 8 g + 7, channels from
-//                 DP/16 i), so that the product with the probabilities needs no
-//                 transposition
-//   value powers  [P/32][DP/32][32]: a lane's eight tokens in one run
-// A token's bytes are its own: tokens can be written in any order.
+// A page holds `page` tokens of every head, head by head; a head's part is a
+// row of records of 32 tokens, so that a wave streams one head's tokens as one
+// run.  A record is laid out as the attention's lanes take it: lane l = 16 g +
+// i reads 16 bytes at 16 l of every kilobyte (piece), so each load of a wave
+// is one run, and both matrix operands come out of the loaded words without an
+// exchange between lanes.  With DP the head size rounded up to 64, 128 or 256:
+//   key values    16 DP bytes.  The key operand's row i of its half a is token
+//                 8 (i / 4) + 4 a + i % 4, and lane (g, i) holds its quarter
+//                 [DP/4 g, DP/4 (g + 1)) of the head: DP/8 bytes for a = 0,
+//                 then for a = 1
+//   value values  16 DP bytes.  Lane (g, i) holds channels [DP/16 i, DP/16 (i +
+//                 1)) of tokens 8 g .. 8 g + 7, DP/32 bytes a token: rows of
+//                 the value operand are channels and its k axis is tokens, so
+//                 the product with the probabilities needs no transposition
+//   key powers    DP bytes: the lane's (where two lanes' quarters share a block,
+//                 the pair's), for a = 0 and then 1
+//   value powers  [DP/32][32] bytes: a lane's eight tokens in one run
+// Channel d of a byte is in its low half for even d.  A token's bytes are its
+// own: tokens can be written in any order.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -52,22 +56,39 @@ struct KvCache {                     // what the kernels need of a cache
     __host__ __device__ size_t page_bytes() const { return head_bytes() * heads; }
 };
 
-// Offsets in one head's part of a page.
+// Offsets in a record.
 template <int DP>
 struct KvLayout {
     static constexpr int kBlocks = DP / kKvBlock;
-    static constexpr int kUnit = DP / 32;       // bytes of a token in one lane's value run
-    static constexpr int kRows = DP / 16;       // channels of a token in one lane's value run
-    __device__ static size_t k_codes(int t) { return (size_t)t * (DP / 2); }
-    __device__ static size_t k_powers(int shift, int t) { return ((size_t)(DP / 2) << shift) + (size_t)t * kBlocks; }
-    __device__ static size_t v_base(int shift) { return (size_t)(DP / 2 + kBlocks) << shift; }
-    // the run of a lane (group g of eight tokens, channels from kRows * i) in the tile of token t
-    __device__ static size_t v_codes(int shift, int tile, int g, int i) {
-        return v_base(shift) + (((size_t)tile * 4 + g) * 16 + i) * 8 * kUnit;
+    static constexpr int kUnit = DP / 32;       // bytes of a token in one lane's values
+    static constexpr int kRows = DP / 16;       // channels of a token in one lane's values
+    static constexpr int kQuarter = DP / 8;     // bytes of a key in one lane
+    static constexpr int kLane = DP / 4;        // bytes of a record's keys (or values) in one lane
+    static constexpr int kPowers = DP == 256 ? 4 : 2;   // key powers of a lane, both halves
+    static constexpr int kRecord = 34 * DP;
+    // byte n of a lane's keys or values
+    __device__ static constexpr int piece(int lane, int n) { return n / 16 * 1024 + lane * 16 + n % 16; }
+    __device__ static constexpr int key_lane_powers(int lane) {
+        return 32 * DP + (DP == 64 ? (lane / 32 * 16 + lane % 16) : lane) * kPowers;
     }
-    __device__ static size_t v_powers(int shift, int tile, int block) {
-        return v_base(shift) + ((size_t)(DP / 2) << shift) + ((size_t)tile * kBlocks + block) * kKvTile;
+    __device__ static constexpr int value_powers(int block) { return 33 * DP + block * kKvTile; }
+    // channels 8 w .. 8 w + 7 of token t: four bytes of a key; four bytes of a
+    // value, or (kUnit 2) two and two in the next lane's
+    __device__ static int key_word(int t, int w) {
+        const int i = t / 8 * 4 + t % 4, n = w * 4;
+        return piece(n / kQuarter * 16 + i, t / 4 % 2 * kQuarter + n % kQuarter);
     }
+    __device__ static int key_power(int t, int block) {
+        const int i = t / 8 * 4 + t % 4, a = t / 4 % 2;
+        if (DP == 64) return 32 * DP + (block * 16 + i) * 2 + a;
+        if (DP == 128) return 32 * DP + (block * 16 + i) * 2 + a;
+        return 32 * DP + ((block / 2 * 16 + i) * 2 + a) * 2 + block % 2;
+    }
+    __device__ static int value_word(int t, int w) {
+        const int d = w * 8;
+        return 16 * DP + piece(t / 8 * 16 + d / kRows, t % 8 * kUnit + d % kRows / 2);
+    }
+    __device__ static int value_power(int t, int block) { return value_powers(block) + t; }
 };
 
 struct KvRows {                      // [b][row][head][dim], the channels contiguous

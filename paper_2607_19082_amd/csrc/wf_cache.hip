@@ -11,9 +11,10 @@ constexpr int kKvThreads = 256;
 
 // ---- kernels ----------------------------------------------------------------
 
-// The head's part of the page that holds token `pos`, or null with the reason
-// in the error word.
-__device__ __forceinline__ uint8_t* kv_page(const KvCache& c, const int* table, int table_pages, int b, int head, int pos) {
+// The head's record that holds token `pos`, or null with the reason in the
+// error word.
+template <int DP>
+__device__ __forceinline__ uint8_t* kv_record(const KvCache& c, const int* table, int table_pages, int b, int head, int pos) {
     const int at = pos >> c.page_shift;
     if (pos < 0 || at >= table_pages) {
         atomicOr(c.err, kErrKvRange);
@@ -24,7 +25,8 @@ __device__ __forceinline__ uint8_t* kv_page(const KvCache& c, const int* table, 
         atomicOr(c.err, kErrKvPage);
         return nullptr;
     }
-    return c.pool + (size_t)page * c.page_bytes() + (size_t)head * c.head_bytes();
+    return c.pool + (size_t)page * c.page_bytes() + (size_t)head * c.head_bytes() +
+           (size_t)((pos & ((1 << c.page_shift) - 1)) / kKvTile) * KvLayout<DP>::kRecord;
 }
 
 template <class T>
@@ -54,16 +56,6 @@ __device__ __forceinline__ void store8(T* p, int m, const float (&x)[8]) {
     }
 }
 
-// Byte offsets of word w (eight channels) of token t of a page: keys hold it
-// as one word; values as one word, or as two halves in neighbouring lanes'
-// runs where a run takes four channels of a token.
-template <int DP>
-__device__ __forceinline__ size_t v_word(int shift, int t, int w) {
-    using L = KvLayout<DP>;
-    const int tile = t / kKvTile, g = t % kKvTile / 8, i = w * 8 / L::kRows;
-    return L::v_codes(shift, tile, g, i) + (size_t)(t % 8) * L::kUnit + (w * 8 % L::kRows) / 2;
-}
-
 // One lane quantises eight channels; four lanes share a block.
 template <int DP, class T>
 __global__ __launch_bounds__(kKvThreads) void k_kv_write(KvCache c, KvRows k, KvRows v, KvTokens a) {
@@ -81,7 +73,7 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_write(KvCache c, KvRows k, Kv
     float x[8] = {};
     if (b < a.B && i < (a.counts ? a.counts[b] : a.n)) {
         pos = a.first[b] + i;
-        base = kv_page(c, a.table, a.table_pages, b, head, pos);
+        base = kv_record<DP>(c, a.table, a.table_pages, b, head, pos);
         const KvRows& s = value ? v : k;
         load8((const T*)s.p + b * s.sb + i * s.sr + head * s.sh + w * 8, c.dim - w * 8, x);
     }
@@ -106,20 +98,20 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_write(KvCache c, KvRows k, Kv
         code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[4] * inv, x[5] * inv, 1.0f, 2);
         code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[6] * inv, x[7] * inv, 1.0f, 3);
     }
-    const int t = pos & ((1 << c.page_shift) - 1);
+    const int t = pos & (kKvTile - 1);
     const uint8_t power = nan ? kKvNan : e + 127;
     if (!value) {
-        *(unsigned*)(base + L::k_codes(t) + w * 4) = code;
-        if (w % 4 == 0) base[L::k_powers(c.page_shift, t) + w / 4] = power;
+        *(unsigned*)(base + L::key_word(t, w)) = code;
+        if (w % 4 == 0) base[L::key_power(t, w / 4)] = power;
     } else {
-        uint8_t* at = base + v_word<DP>(c.page_shift, t, w);
+        uint8_t* at = base + L::value_word(t, w);
         if constexpr (L::kRows == 4) {
             *(uint16_t*)at = (uint16_t)code;
-            *(uint16_t*)(at + 8 * L::kUnit) = (uint16_t)(code >> 16);
+            *(uint16_t*)(at + 16) = (uint16_t)(code >> 16);
         } else {
             *(unsigned*)at = code;
         }
-        if (w % 4 == 0) base[L::v_powers(c.page_shift, t / kKvTile, w / 4) + t % kKvTile] = power;
+        if (w % 4 == 0) base[L::value_power(t, w / 4)] = power;
     }
 }
 
@@ -142,18 +134,18 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_read(KvCache c, KvRows k, KvR
     T* out = (T*)s.p + b * s.sb + i * s.sr + head * s.sh + w * 8;
     float x[8] = {};
     if (i < (a.counts ? a.counts[b] : a.n)) {
-        const int pos = a.first[b] + i, t = pos & ((1 << c.page_shift) - 1);
-        const uint8_t* base = kv_page(c, a.table, a.table_pages, b, head, pos);
+        const int pos = a.first[b] + i, t = pos & (kKvTile - 1);
+        const uint8_t* base = kv_record<DP>(c, a.table, a.table_pages, b, head, pos);
         if (base) {
             unsigned code, power;
             if (!value) {
-                code = *(const unsigned*)(base + L::k_codes(t) + w * 4);
-                power = base[L::k_powers(c.page_shift, t) + w / 4];
+                code = *(const unsigned*)(base + L::key_word(t, w));
+                power = base[L::key_power(t, w / 4)];
             } else {
-                const uint8_t* at = base + v_word<DP>(c.page_shift, t, w);
-                if constexpr (L::kRows == 4) code = *(const uint16_t*)at | (unsigned)*(const uint16_t*)(at + 8 * L::kUnit) << 16;
+                const uint8_t* at = base + L::value_word(t, w);
+                if constexpr (L::kRows == 4) code = *(const uint16_t*)at | (unsigned)*(const uint16_t*)(at + 16) << 16;
                 else code = *(const unsigned*)at;
-                power = base[L::v_powers(c.page_shift, t / kKvTile, w / 4) + t % kKvTile];
+                power = base[L::value_power(t, w / 4)];
             }
             const float scale = __builtin_bit_cast(float, power << 23);   // 255: the conversion gives NaN
 #define WF_PAIR(j)                                                                    \
