@@ -30,8 +30,11 @@ namespace wf {
 
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef float f2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
-typedef unsigned u2 __attribute__((ext_vector_type(2)));
+// read-only for the whole launch, at addresses that a wave shares: scalar loads
+typedef const int __attribute__((address_space(4))) * SharedInts;
 
 constexpr int kAtWaves = 4;
 constexpr int kAtThreads = 64 * kAtWaves;
@@ -52,17 +55,26 @@ struct AtParts<float> {
 
 __device__ __forceinline__ f4 mfma(b8 a, b8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-// Eight values as N bf16 parts, the largest first.
+// Eight values as N bf16 parts, the largest first.  What a part leaves is one
+// dot product: r - 1 * part + 0 * its neighbour, exact.  The pairs (-1, 0) and
+// (0, -1) come from registers: as an instruction's own constant, -1 stands for
+// the other pair.
 template <int N>
 __device__ __forceinline__ void parts(const float (&x)[8], b8 (&p)[N]) {
+    unsigned first = 0x0000bf80u, second = 0xbf800000u;
+    asm("" : "+s"(first), "+s"(second));
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        float r = x[e];
+    for (int e = 0; e < 8; e += 2) {
+        f2 r = {x[e], x[e + 1]};
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const __bf16 h = (__bf16)r;
-            p[n][e] = h;
-            r -= (float)h;
+            const b2 h = __builtin_convertvector(r, b2);
+            p[n][e] = h[0];
+            p[n][e + 1] = h[1];
+            if (n + 1 < N) {
+                r[0] = __builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(b2, first), r[0], false);
+                r[1] = __builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(b2, second), r[1], false);
+            }
         }
     }
 }
@@ -230,13 +242,13 @@ __global__ __launch_bounds__(kAtThreads, (kAtWgs<DP, T, NT>)) void k_attend(Atte
     const int tiles = (most + kKvTile - 1) / kKvTile;
     const int share = (tiles + a.splits - 1) / a.splits;
     const int t0 = split * share, t1 = min(tiles, t0 + share);
-    const int* table = a.table + (size_t)b * a.table_pages;
+    const SharedInts table = (SharedInts)(a.table + (size_t)b * a.table_pages);
     const int in_page = a.c.page_shift - 5;
     const uint8_t* pool = a.c.pool + (size_t)head * a.c.head_bytes();
     const size_t page_bytes = a.c.page_bytes();
 
     f4 o[NT][ND], l[NT], bad[NT];
-    float m[NT], sub[NT];
+    float m[NT], sub[NT], raise[NT];       // maximum; what is subtracted; where it is raised
     b8 ones;
 #pragma unroll
     for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.0f;
@@ -251,12 +263,11 @@ __global__ __launch_bounds__(kAtThreads, (kAtWgs<DP, T, NT>)) void k_attend(Atte
 #pragma unroll
             for (int r = 0; r < ND; ++r) o[t][r] = f4{0, 0, 0, 0};
             l[t] = bad[t] = f4{0, 0, 0, 0};
-            m[t] = -INFINITY;
+            m[t] = raise[t] = -INFINITY;
             sub[t] = 0.0f;
         }
         AtTile<DP> buf[2];
-        auto load = [&](AtTile<DP>& x, int tile) {
-            const int page = table[tile >> in_page];
+        auto load = [&](AtTile<DP>& x, int tile, int page) {
             const bool there = page >= 0 && page < a.c.pages;
             load_tile<DP>(x, pool + (size_t)(there ? page : 0) * page_bytes + (size_t)(tile & ((1 << in_page) - 1)) * L::kRecord, lane);
             return there;
@@ -268,62 +279,65 @@ __global__ __launch_bounds__(kAtThreads, (kAtWgs<DP, T, NT>)) void k_attend(Atte
             add_scores<DP, NT, NQ, 0>(x, q, s);
             add_scores<DP, NT, NQ, 1>(x, q, s);
             const int at = tile * kKvTile + 8 * g;         // the lane's first token
-            const bool whole = !MASK && (tile + 1) * kKvTile <= least;
-            unsigned char sees[NT];
+            const bool edge = MASK || care || (tile + 1) * kKvTile > least;   // some row may not see all of it
+            unsigned sees[NT];
+            if (edge) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                sees[t] = 0xff;
-                if (!whole) {
+                for (int t = 0; t < NT; ++t) {
+                    const int left = see[t] - at;
                     sees[t] = 0;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        bool on = at + e < see[t];
+                        bool on = e < left;
                         if constexpr (MASK) on = on && mask[t][at + e];
-                        sees[t] |= on << e;
+                        sees[t] |= (unsigned)on << e;
                         s[t][e / 4][e % 4] = on ? s[t][e / 4][e % 4] : -INFINITY;
                     }
                 }
             }
             float power[8] = {power_at<0>(x.vp[0]), power_at<1>(x.vp[0]), power_at<2>(x.vp[0]), power_at<3>(x.vp[0]),
                               power_at<0>(x.vp[1]), power_at<1>(x.vp[1]), power_at<2>(x.vp[1]), power_at<3>(x.vp[1])};
-            if ((tile + 1) * kKvTile > most) {
+            if (edge) {
                 // past the last token that any row sees, a page holds anything
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (at + e >= most) power[e] = 1.0f;
-            }
-            if (care) {
-                unsigned spoilt = 0;
+                    if (e >= most - at) power[e] = 1.0f;
+                if (care) {
+                    unsigned spoilt = 0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (power[e] == INFINITY) {
-                        spoilt |= 1u << e;
-                        power[e] = 1.0f;
+                    for (int e = 0; e < 8; ++e)
+                        if (power[e] == INFINITY) {
+                            spoilt |= 1u << e;
+                            power[e] = 1.0f;
+                        }
+                    b8 is;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) is[e] = (__bf16)(float)(spoilt >> e & 1);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        b8 on;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) on[e] = (__bf16)(float)(sees[t] >> e & 1);
+                        bad[t] = mfma(is, on, bad[t]);
                     }
-                b8 is;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) is[e] = (__bf16)(float)(spoilt >> e & 1);
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    b8 on;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) on[e] = (__bf16)(float)(sees[t] >> e & 1);
-                    bad[t] = mfma(is, on, bad[t]);
                 }
             }
             b8 p[NT][NP];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
+                // NaN where a score is: the row's maximum then stays as it is,
+                // and its outputs become NaN through the exponent
                 float top = s[t][0][0];
 #pragma unroll
-                for (int e = 1; e < 8; ++e) top = fmaxf(top, s[t][e / 4][e % 4]);
+                for (int e = 1; e < 8; ++e) top = __builtin_elementwise_maximum(top, s[t][e / 4][e % 4]);
                 top *= a.scale_log2;
-                if (__any(top > (m[t] == -INFINITY ? -INFINITY : m[t] + kAtSlack))) {
+                if (__any(top > raise[t])) {
                     top = fmaxf(top, __shfl_xor(top, 16));
                     top = fmaxf(top, __shfl_xor(top, 32));
                     const float next = fmaxf(m[t], top), by = m[t] == -INFINITY ? 0.0f : exp2f(m[t] - next);
                     if (next != -INFINITY) {
                         m[t] = sub[t] = next;
+                        raise[t] = next + kAtSlack;
 #pragma unroll
                         for (int r = 0; r < ND; ++r) o[t][r] *= by;
                         l[t] *= by;
@@ -338,17 +352,29 @@ __global__ __launch_bounds__(kAtThreads, (kAtWgs<DP, T, NT>)) void k_attend(Atte
             }
             add_values<DP, NT, NP>(x.v, power, p, o);
         };
-        // the next tile is loaded while this one is worked on
+        // The next tile is loaded while one is worked on, and the page of the
+        // one after it; past the end it is the last one again, so that the
+        // loads in flight are the same on every path.
         int tile = t0 + wave;
-        bool there[2] = {tile < t1 && load(buf[0], tile), false};
-        while (tile < t1) {
+        if (tile < t1) {
+            auto page_of = [&](int t) { return table[min(t, t1 - 1) >> in_page]; };
+            int page = page_of(tile);
+            bool there[2];
+            there[0] = load(buf[0], tile, page);
+            page = page_of(tile + kAtWaves);
+            while (tile < t1) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                if (tile >= t1) break;
-                there[1 - h] = tile + kAtWaves < t1 && load(buf[1 - h], tile + kAtWaves);
-                if (there[h]) take(buf[h], tile);
-                else if (lane == 0) atomicOr(a.c.err, kErrKvPage);
-                tile += kAtWaves;
+                for (int h = 0; h < 2; ++h) {
+                    there[1 - h] = load(buf[1 - h], min(tile + kAtWaves, t1 - 1), page);
+                    page = page_of(tile + 2 * kAtWaves);
+                    if (!there[h]) {
+                        if (lane == 0) atomicOr(a.c.err, kErrKvPage);
+                    } else {
+                        take(buf[h], tile);
+                    }
+                    tile += kAtWaves;
+                    if (tile >= t1) break;
+                }
             }
         }
         if (care) break;
