@@ -30,14 +30,19 @@ namespace wf {
 
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef float f8 __attribute__((ext_vector_type(8)));
 typedef float f2 __attribute__((ext_vector_type(2)));
 typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
+typedef unsigned u2 __attribute__((ext_vector_type(2)));
 // read-only for the whole launch, at addresses that a wave shares: scalar loads
 typedef const int __attribute__((address_space(4))) * SharedInts;
 
-constexpr int kAtWaves = 4;
-constexpr int kAtThreads = 64 * kAtWaves;
+constexpr int kAtTarget = 256;      // workgroups that a call is split into
+constexpr int kAtJoin = 256;        // threads of the kernel that joins the splits
+// waves of a workgroup
+template <int DP, class T, int NT>
+constexpr int kAtWaves = NT == 1 && DP * sizeof(T) < 1024 ? 8 : 4;
 // a row's maximum is raised only when a score passes it by this much (in
 // powers of two): its probabilities then stay below 2^8
 constexpr float kAtSlack = 8.0f;
@@ -178,22 +183,36 @@ __device__ __forceinline__ void add_values(const unsigned (&v)[DP / 16], const f
     }
 }
 
-// Workgroups of a compute unit that the registers are shared out for.
+// Weight of a partial result with maximum m and sum l; 0 where it saw no token.
+__device__ __forceinline__ float at_weight(float m, float l, float most) {
+    return m == -INFINITY && l == 0.0f ? 0.0f : (m == most ? 1.0f : exp2f(m - most));
+}
+
+// Eight channels of a row, into the output.
+template <class T>
+__device__ __forceinline__ void write_row(const AttendArgs& a, int b, int head, int row, int d, const f8& v) {
+    const int i = row / a.group, h = head * a.group + row % a.group;
+    T out[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) out[e] = (T)v[e];
+    __builtin_memcpy((T*)a.o.p + b * a.o.sb + i * a.o.sr + h * a.o.sh + d, out, sizeof out);
+}
+
+// Waves of a SIMD that the registers are shared out for.
 template <int DP, class T, int NT>
 constexpr int kAtWgs = NT * DP * (int)sizeof(T) <= 128 * 2 ? 3 : (NT * DP * (int)sizeof(T) <= 256 * 2 ? 2 : 1);
 
 // One workgroup: 16 NT rows of a sequence's key head, and a share of its
 // tokens.
 template <int DP, class T, int NT, bool MASK>
-__global__ __launch_bounds__(kAtThreads, (kAtWgs<DP, T, NT>)) void k_attend(AttendArgs a) {
-    constexpr int NQ = AtParts<T>::kQ, NP = AtParts<T>::kP, NK = DP / 32, ND = DP / 16;
+__global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) void k_attend(AttendArgs a) {
+    constexpr int NW = kAtWaves<DP, T, NT>, NQ = AtParts<T>::kQ, NP = AtParts<T>::kP, NK = DP / 32, ND = DP / 16;
     using L = KvLayout<DP>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int rows = a.n * a.group, nrt = (rows + 16 * NT - 1) / (16 * NT);
-    int id = blockIdx.x;
-    const int split = id % a.splits; id /= a.splits;
-    const int rt = nrt - 1 - id % nrt; id /= nrt;      // under a causal order the last rows see most: first
-    const int head = id % a.c.heads, b = id / a.c.heads;
+    const int split = blockIdx.x % a.splits, group = blockIdx.x / a.splits;
+    const int rt = nrt - 1 - group % nrt;              // under a causal order the last rows see most: first
+    const int head = group / nrt % a.c.heads, b = group / nrt / a.c.heads;
 
     // the lane's rows: their queries, and how many tokens they see
     b8 q[NT][NK][NQ];
@@ -267,12 +286,26 @@ __global__ __launch_bounds__(kAtThreads, (kAtWgs<DP, T, NT>)) void k_attend(Atte
             sub[t] = 0.0f;
         }
         AtTile<DP> buf[2];
-        auto load = [&](AtTile<DP>& x, int tile, int page) {
+        u2 allow[2][NT];                   // the mask's bytes of the lane's tokens
+        auto load = [&](AtTile<DP>& x, u2 (&allow)[NT], int tile, int page) {
             const bool there = page >= 0 && page < a.c.pages;
+            if constexpr (MASK) {
+                const int at = tile * kKvTile + 8 * g;
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    if (at + 8 <= a.max_visible) {
+                        __builtin_memcpy(&allow[t], mask[t] + at, 8);
+                    } else {
+                        uint64_t x = 0;
+                        for (int e = 0; at + e < a.max_visible; ++e) x |= (uint64_t)mask[t][at + e] << 8 * e;
+                        allow[t] = __builtin_bit_cast(u2, x);
+                    }
+                }
+            }
             load_tile<DP>(x, pool + (size_t)(there ? page : 0) * page_bytes + (size_t)(tile & ((1 << in_page) - 1)) * L::kRecord, lane);
             return there;
         };
-        auto take = [&](const AtTile<DP>& x, int tile) {
+        auto take = [&](const AtTile<DP>& x, const u2 (&allow)[NT], int tile) {
             f4 s[NT][2];
 #pragma unroll
             for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = f4{0, 0, 0, 0};
@@ -289,7 +322,7 @@ __global__ __launch_bounds__(kAtThreads, (kAtWgs<DP, T, NT>)) void k_attend(Atte
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         bool on = e < left;
-                        if constexpr (MASK) on = on && mask[t][at + e];
+                        if constexpr (MASK) on = on && (allow[t][e / 4] >> 8 * (e % 4) & 0xff);
                         sees[t] |= (unsigned)on << e;
                         s[t][e / 4][e % 4] = on ? s[t][e / 4][e % 4] : -INFINITY;
                     }
@@ -360,19 +393,19 @@ __global__ __launch_bounds__(kAtThreads, (kAtWgs<DP, T, NT>)) void k_attend(Atte
             auto page_of = [&](int t) { return table[min(t, t1 - 1) >> in_page]; };
             int page = page_of(tile);
             bool there[2];
-            there[0] = load(buf[0], tile, page);
-            page = page_of(tile + kAtWaves);
+            there[0] = load(buf[0], allow[0], tile, page);
+            page = page_of(tile + NW);
             while (tile < t1) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    there[1 - h] = load(buf[1 - h], min(tile + kAtWaves, t1 - 1), page);
-                    page = page_of(tile + 2 * kAtWaves);
+                    there[1 - h] = load(buf[1 - h], allow[1 - h], min(tile + NW, t1 - 1), page);
+                    page = page_of(tile + 2 * NW);
                     if (!there[h]) {
                         if (lane == 0) atomicOr(a.c.err, kErrKvPage);
                     } else {
-                        take(buf[h], tile);
+                        take(buf[h], allow[h], tile);
                     }
-                    tile += kAtWaves;
+                    tile += NW;
                     if (tile >= t1) break;
                 }
             }
@@ -396,12 +429,14 @@ __global__ __launch_bounds__(kAtThreads, (kAtWgs<DP, T, NT>)) void k_attend(Atte
                 for (int r = 0; r < ND; ++r) o[t][r][e] = __builtin_nanf("");
 
     // join the waves, one tile of 16 rows after the other
-    constexpr int kPitch = DP + 4;
-    __shared__ float so[kAtWaves][16 * kPitch];
-    __shared__ float sm[kAtWaves][16], sl[kAtWaves][16];
+    constexpr int kPitch = DP + 4, W = DP / 8, kThreads = 64 * NW;
+    __shared__ float lds[NW * 16 * kPitch];
+    __shared__ float sm[NW][16], sl[NW][16], top[16];
+    const int row0 = rt * 16 * NT, here = min(16 * NT, rows - row0);
+    const size_t part = ((size_t)group * a.splits + split) * 16 * NT;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        __syncthreads();
+        if (t) __syncthreads();
         if (lane < 16) {
             sm[wave][lane] = m[t];
             sl[wave][lane] = l[t][0];
@@ -410,37 +445,47 @@ __global__ __launch_bounds__(kAtThreads, (kAtWgs<DP, T, NT>)) void k_attend(Atte
         for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int r = 0; r < ND; r += 4)
-                *(f4*)&so[wave][col * kPitch + ND * (4 * g + e) + r] = f4{o[t][r][e], o[t][r + 1][e], o[t][r + 2][e], o[t][r + 3][e]};
+                *(f4*)&lds[(wave * 16 + col) * kPitch + ND * (4 * g + e) + r] =
+                    f4{o[t][r][e], o[t][r + 1][e], o[t][r + 2][e], o[t][r + 3][e]};
         __syncthreads();
-        for (int x = threadIdx.x; x < 16 * DP / 8; x += kAtThreads) {
-            const int c = x / (DP / 8), d = x % (DP / 8) * 8, row = rt * 16 * NT + t * 16 + c;
-            if (row >= rows) continue;
-            float top = sm[0][c], sum = 0.0f, v[8] = {};
+        if (threadIdx.x < 16) {
+            // each wave's weight, with the sum's inverse in it where the row
+            // is complete
+            const int c = threadIdx.x;
+            float most = sm[0][c], sum = 0.0f, by[NW];
 #pragma unroll
-            for (int w = 1; w < kAtWaves; ++w) top = fmaxf(top, sm[w][c]);
+            for (int w = 1; w < NW; ++w) most = fmaxf(most, sm[w][c]);
 #pragma unroll
-            for (int w = 0; w < kAtWaves; ++w) {
-                if (sm[w][c] == -INFINITY && sl[w][c] == 0.0f) continue;      // it saw no token
-                const float by = sm[w][c] == top ? 1.0f : exp2f(sm[w][c] - top);
-                sum += by * sl[w][c];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += by * so[w][c * kPitch + d + e];
+            for (int w = 0; w < NW; ++w) {
+                by[w] = at_weight(sm[w][c], sl[w][c], most);
+                sum += by[w] * sl[w][c];
             }
-            const int i = row / a.group, h = head * a.group + row % a.group;
-            if (a.splits == 1) {
-                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                if (d < a.c.dim) {
-                    T out[8];
+            const float scale = a.splits > 1 ? 1.0f : (sum == 0.0f ? 0.0f : 1.0f / sum);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) out[e] = (T)(v[e] * inv);
-                    __builtin_memcpy((T*)a.o.p + b * a.o.sb + i * a.o.sr + h * a.o.sh + d, out, sizeof out);
-                }
+            for (int w = 0; w < NW; ++w) sm[w][c] = by[w] * scale;
+            top[c] = most;
+            sl[0][c] = sum;
+        }
+        __syncthreads();
+        for (int x = threadIdx.x; x < min(16, here - t * 16) * W; x += kThreads) {
+            const int c = x / W, d = x % W * 8;
+            f8 v = {};
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                f8 y;
+                __builtin_memcpy(&y, __builtin_assume_aligned(&lds[(w * 16 + c) * kPitch + d], 16), sizeof y);
+                const float by = sm[w][c];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += by * y[e];
+            }
+            if (a.splits == 1) {
+                if (d < a.c.dim) write_row<T>(a, b, head, row0 + t * 16 + c, d, v);
             } else {
-                const size_t at = (((size_t)b * a.n + i) * (a.c.heads * a.group) + h) * a.splits + split;
-                __builtin_memcpy(a.part_o + at * DP + d, v, sizeof v);
+                const size_t at = part + t * 16 + c;
+                __builtin_memcpy(__builtin_assume_aligned(a.part_o + at * DP + d, 16), &v, sizeof v);
                 if (d == 0) {
-                    a.part_ml[at * 2] = top;
-                    a.part_ml[at * 2 + 1] = sum;
+                    const f2 z = {top[c], sl[0][c]};
+                    __builtin_memcpy(__builtin_assume_aligned(a.part_ml + at * 2, 8), &z, sizeof z);
                 }
             }
         }
@@ -450,15 +495,15 @@ __global__ __launch_bounds__(kAtThreads, (kAtWgs<DP, T, NT>)) void k_attend(Atte
 // Joins the splits of one row: eight channels a lane, the splits dealt to
 // groups of lanes that join at the end.
 template <int DP, class T>
-__global__ __launch_bounds__(kAtThreads) void k_attend_join(AttendArgs a) {
-    constexpr int W = DP / 8, G = kAtThreads / W;
+__global__ __launch_bounds__(kAtJoin) void k_attend_join(AttendArgs a, int tile_rows) {
+    constexpr int W = DP / 8, G = kAtJoin / W;
     __shared__ float so[G][DP], sm[G], sl[G];
-    const long long row = blockIdx.x;
-    const int d = threadIdx.x % W * 8, g = threadIdx.x / W, hq = a.c.heads * a.group;
-    const float* ml = a.part_ml + row * a.splits * 2;
-    const float* po = a.part_o + row * a.splits * DP + d;
-    float top = -INFINITY, sum = 0.0f, v[8] = {};
-    auto add = [&](float m, float l, const float* x) {
+    const int rows = a.n * a.group, row = blockIdx.x % rows, bh = blockIdx.x / rows, g = threadIdx.x / W, d = threadIdx.x % W * 8;
+    const int nrt = (rows + tile_rows - 1) / tile_rows;
+    const size_t first = ((size_t)bh * nrt + (nrt - 1 - row / tile_rows)) * a.splits * tile_rows + row % tile_rows;
+    float top = -INFINITY, sum = 0.0f;
+    f8 v = {};
+    auto add = [&](float m, float l, const f8& x) {
         if (m == -INFINITY && l == 0.0f) return;         // it saw no token
         const float next = fmaxf(top, m), old = top == next ? 1.0f : exp2f(top - next), by = m == next ? 1.0f : exp2f(m - next);
         sum = old * sum + by * l;
@@ -466,80 +511,94 @@ __global__ __launch_bounds__(kAtThreads) void k_attend_join(AttendArgs a) {
         for (int e = 0; e < 8; ++e) v[e] = old * v[e] + by * x[e];
         top = next;
     };
-    for (int s = g; s < a.splits; s += G) {
-        float x[8];
-        __builtin_memcpy(x, __builtin_assume_aligned(po + (size_t)s * DP, 16), sizeof x);
-        add(ml[2 * s], ml[2 * s + 1], x);
+    for (int s = g; s < a.splits; s += 4 * G) {
+        f2 z[4];
+        f8 y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const size_t at = first + (size_t)min(s + j * G, a.splits - 1) * tile_rows;
+            __builtin_memcpy(&z[j], __builtin_assume_aligned(a.part_ml + at * 2, 8), 8);
+            __builtin_memcpy(&y[j], __builtin_assume_aligned(a.part_o + at * DP + d, 16), 32);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (s + j * G < a.splits) add(z[j][0], z[j][1], y[j]);
     }
-    __builtin_memcpy(&so[g][d], v, sizeof v);
+    __builtin_memcpy(__builtin_assume_aligned(&so[g][d], 16), &v, 32);
     if (d == 0) {
         sm[g] = top;
         sl[g] = sum;
     }
     __syncthreads();
     if (g || d >= a.c.dim) return;
-    for (int j = 1; j < G; ++j) add(sm[j], sl[j], &so[j][d]);
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    const int h = row % hq;
-    const long long bi = row / hq;
-    T out[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) out[e] = (T)(v[e] * inv);
-    __builtin_memcpy((T*)a.o.p + bi / a.n * a.o.sb + bi % a.n * a.o.sr + h * a.o.sh + d, out, sizeof out);
+    for (int j = 1; j < min(G, a.splits); ++j) {
+        f8 y;
+        __builtin_memcpy(&y, __builtin_assume_aligned(&so[j][d], 16), 32);
+        add(sm[j], sl[j], y);
+    }
+    v *= sum == 0.0f ? 0.0f : 1.0f / sum;
+    write_row<T>(a, bh / a.c.heads, bh % a.c.heads, row, d, v);
 }
 
 // ---- host -----------------------------------------------------------------------
 
-// Column tiles of a workgroup.
+// Column tiles of a workgroup: two where they fit the registers without spills
+// and there are enough rows to fill the chip all the same.  us with one / two, 8
+// heads of 128, 16384 tokens, bf16: 64 tiles 28 / 30, 256 78 / 77, 512 149 /
+// 130, 2048 520 / 393; 5 heads of 64, 8192 tokens, fp32: 20 tiles 15 / 19, 160
+// 47 / 40, 320 71 / 66.  (Two of 128 channels in fp32 gain nothing: 2048 tiles
+// 382 / 385; nor do four of 64 in bf16: 320 tiles 49 / 50, four 52.)
+template <int DP, class T>
+constexpr bool kAtTwoTiles = DP * sizeof(T) <= 256;
+constexpr long long kAtManyTiles = 512;
+
 static int row_tiles(const AttendArgs& a, int precision) {
-    const int rows = a.n * a.group, most = precision == WF_FP32 ? (a.c.dp == 256 ? 1 : 2) : (a.c.dp == 256 ? 2 : 4);
-    return rows <= 16 || most == 1 ? 1 : (rows <= 32 || most == 2 ? 2 : 4);
+    const long long tiles = (long long)a.B * a.c.heads * ((a.n * a.group + 15) / 16);
+    return tiles >= kAtManyTiles && a.c.dp * (precision == WF_BF16 ? 2 : 4) <= 256 ? 2 : 1;
 }
 
-long long attend_plan(AttendArgs& a, int precision) {
-    const int nt = row_tiles(a, precision), rows = a.n * a.group;
+void attend_plan(AttendArgs& a, int precision) {
+    const int nt = row_tiles(a, precision), rows = a.n * a.group, waves = nt == 1 && (precision == WF_BF16 || a.c.dp < 256) ? 8 : 4;
     const long long groups = (long long)a.B * a.c.heads * ((rows + 16 * nt - 1) / (16 * nt));
-    const long long all = (long long)a.B * a.n * a.c.heads * a.group;
-    // workgroups that keep the chip busy, with at least two tiles for each wave
-    long long s = (1024 + groups - 1) / groups;
-    const long long by_len = a.max_visible / (2 * kAtWaves * kKvTile);
+    // workgroups that keep the chip busy, with at least four tiles for each wave
+    long long s = (kAtTarget + groups - 1) / groups;
+    const long long by_len = a.max_visible / (4 * waves * kKvTile);
     s = s < by_len ? s : by_len;
-    const long long by_room = kAttendWorkRows / all;
+    const long long by_room = kAttendWorkRows / (groups * 16 * nt);
     s = s < by_room ? s : by_room;
     a.splits = s < 2 ? 1 : (int)s;
-    return a.splits == 1 ? 0 : all * a.splits;
 }
 
 template <int DP, class T, int NT>
 static void launch_nt(const AttendArgs& a, hipStream_t st) {
     const int rows = a.n * a.group;
     const long long groups = (long long)a.B * a.c.heads * ((rows + 16 * NT - 1) / (16 * NT));
+    constexpr int kThreads = 64 * kAtWaves<DP, T, NT>;
     const dim3 grid((unsigned)(groups * a.splits));
-    if (a.mask) hipLaunchKernelGGL((k_attend<DP, T, NT, true>), grid, dim3(kAtThreads), 0, st, a);
-    else hipLaunchKernelGGL((k_attend<DP, T, NT, false>), grid, dim3(kAtThreads), 0, st, a);
-    if (a.splits > 1) {
-        const long long all = (long long)a.B * a.n * a.c.heads * a.group;
-        hipLaunchKernelGGL((k_attend_join<DP, T>), dim3((unsigned)all), dim3(kAtThreads), 0, st, a);
-    }
+    if (a.mask) hipLaunchKernelGGL((k_attend<DP, T, NT, true>), grid, dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL((k_attend<DP, T, NT, false>), grid, dim3(kThreads), 0, st, a);
+    if (a.splits > 1)
+        hipLaunchKernelGGL((k_attend_join<DP, T>), dim3((unsigned)(a.B * a.c.heads * rows)), dim3(kAtJoin), 0, st, a, 16 * NT);
 }
 
-template <int DP>
-static void launch_dp(const AttendArgs& a, int precision, hipStream_t st) {
-    const int nt = row_tiles(a, precision);
-    if (precision == WF_BF16) {
-        if (nt == 1) launch_nt<DP, __bf16, 1>(a, st);
-        else if (nt == 2) launch_nt<DP, __bf16, 2>(a, st);
-        else if constexpr (DP < 256) launch_nt<DP, __bf16, 4>(a, st);
-    } else {
-        if (nt == 1) launch_nt<DP, float, 1>(a, st);
-        else if constexpr (DP < 256) launch_nt<DP, float, 2>(a, st);
-    }
+template <int DP, class T>
+static void launch_dp(const AttendArgs& a, int nt, hipStream_t st) {
+    if constexpr (kAtTwoTiles<DP, T>)
+        if (nt == 2) return launch_nt<DP, T, 2>(a, st);
+    launch_nt<DP, T, 1>(a, st);
+}
+
+template <class T>
+static void launch_precision(const AttendArgs& a, int nt, hipStream_t st) {
+    if (a.c.dp == 64) launch_dp<64, T>(a, nt, st);
+    else if (a.c.dp == 128) launch_dp<128, T>(a, nt, st);
+    else launch_dp<256, T>(a, nt, st);
 }
 
 void launch_attend(const AttendArgs& a, int precision, hipStream_t st) {
-    if (a.c.dp == 64) launch_dp<64>(a, precision, st);
-    else if (a.c.dp == 128) launch_dp<128>(a, precision, st);
-    else launch_dp<256>(a, precision, st);
+    const int nt = row_tiles(a, precision);
+    if (precision == WF_BF16) launch_precision<__bf16>(a, nt, st);
+    else launch_precision<float>(a, nt, st);
 }
 
 }  // namespace wf

@@ -110,14 +110,13 @@ struct AttendArgs {
     int table_pages, B, n, group;    // group: query heads of a key head
     int max_visible, splits;
     float scale_log2;                // scale * log2(e)
-    float *part_o, *part_ml;
+    float *part_o, *part_ml;         // partial results: channels, and (maximum, sum)
 };
 
 void launch_kv_write(const KvCache&, int precision, const KvRows& k, const KvRows& v, const KvTokens&, hipStream_t);
 void launch_kv_read(const KvCache&, int precision, const KvRows& k, const KvRows& v, const KvTokens&, hipStream_t);
-// Splits of a call and the rows of partial results that it leaves in the
-// workspace (0: the kernel writes the output itself).
-long long attend_plan(AttendArgs&, int precision);
+// The splits of a call, so that its partial results fit the workspace.
+void attend_plan(AttendArgs&, int precision);
 void launch_attend(const AttendArgs&, int precision, hipStream_t);
 
 }  // namespace wf

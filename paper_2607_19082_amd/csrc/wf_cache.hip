@@ -191,7 +191,6 @@ void launch_kv_read(const KvCache& c, int precision, const KvRows& k, const KvRo
 struct Cache {
     KvCache c{};
     float* work = nullptr;           // partial results of split attention calls
-    long long work_rows = 0;
 };
 
 static int kv_fail(hipError_t e, const char* what) { return fail(WF_E_HIP, std::string(what) + ": " + hipGetErrorString(e)); }
@@ -251,10 +250,9 @@ int wf_cache_plan(const wf_cache_desc* d, wf_cache_t* out) {
     k.dp = d->dim <= 64 ? 64 : (d->dim <= 128 ? 128 : 256);
     while ((1 << k.page_shift) < d->page) ++k.page_shift;
     const size_t bytes = k.page_bytes() * k.pages;
-    c->work_rows = kAttendWorkRows;
     hipError_t e = hipMalloc((void**)&k.pool, bytes);
     if (e == hipSuccess) e = hipMalloc((void**)&k.err, sizeof(int));
-    if (e == hipSuccess) e = hipMalloc((void**)&c->work, (size_t)c->work_rows * (k.dp + 2) * sizeof(float));
+    if (e == hipSuccess) e = hipMalloc((void**)&c->work, (size_t)kAttendWorkRows * (k.dp + 2) * sizeof(float));
     if (e != hipSuccess) {
         free_cache(c);
         return fail(WF_E_NOMEM, std::string("cache: ") + hipGetErrorString(e));
@@ -322,10 +320,9 @@ int wf_cache_attend(wf_cache_t cache, int32_t precision, const wf_rows* q, const
     a.table_pages = table_pages; a.B = B; a.n = n; a.group = q_heads / c->c.heads;
     a.max_visible = max_visible;
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
-    const long long rows = attend_plan(a, precision);
-    if (rows > c->work_rows) return fail(WF_E_UNSUPPORTED, "the call does not fit the workspace");
+    attend_plan(a, precision);
     a.part_o = c->work;
-    a.part_ml = c->work + (size_t)rows * c->c.dp;
+    a.part_ml = c->work + (size_t)kAttendWorkRows * c->c.dp;
     launch_attend(a, precision, stream);
     return kv_launched("wf_cache_attend");
 }
