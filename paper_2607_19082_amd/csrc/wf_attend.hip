@@ -553,8 +553,9 @@ constexpr bool kAtTwoTiles = DP * sizeof(T) <= 256;
 constexpr long long kAtManyTiles = 512;
 
 static int row_tiles(const AttendArgs& a, int precision) {
-    const long long tiles = (long long)a.B * a.c.heads * ((a.n * a.group + 15) / 16);
-    return tiles >= kAtManyTiles && a.c.dp * (precision == WF_BF16 ? 2 : 4) <= 256 ? 2 : 1;
+    const int rows = a.n * a.group;
+    const long long tiles = (long long)a.B * a.c.heads * ((rows + 15) / 16);
+    return rows > 16 && tiles >= kAtManyTiles && a.c.dp * (precision == WF_BF16 ? 2 : 4) <= 256 ? 2 : 1;
 }
 
 void attend_plan(AttendArgs& a, int precision) {

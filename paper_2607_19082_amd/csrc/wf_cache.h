@@ -72,20 +72,18 @@ struct KvLayout {
         return 32 * DP + (DP == 64 ? (lane / 32 * 16 + lane % 16) : lane) * kPowers;
     }
     __device__ static constexpr int value_powers(int block) { return 33 * DP + block * kKvTile; }
-    // channels 8 w .. 8 w + 7 of token t: four bytes of a key; four bytes of a
-    // value, or (kUnit 2) two and two in the next lane's
-    __device__ static int key_word(int t, int w) {
-        const int i = t / 8 * 4 + t % 4, n = w * 4;
+    // byte of channels d, d + 1 of token t; of a value, a lane's run ends after
+    // kRows channels and the next lane's follows 16 bytes on (kUnit 2)
+    __device__ static int key_at(int t, int d) {
+        const int i = t / 8 * 4 + t % 4, n = d / 2;
         return piece(n / kQuarter * 16 + i, t / 4 % 2 * kQuarter + n % kQuarter);
     }
     __device__ static int key_power(int t, int block) {
         const int i = t / 8 * 4 + t % 4, a = t / 4 % 2;
-        if (DP == 64) return 32 * DP + (block * 16 + i) * 2 + a;
-        if (DP == 128) return 32 * DP + (block * 16 + i) * 2 + a;
+        if (DP < 256) return 32 * DP + (block * 16 + i) * 2 + a;
         return 32 * DP + ((block / 2 * 16 + i) * 2 + a) * 2 + block % 2;
     }
-    __device__ static int value_word(int t, int w) {
-        const int d = w * 8;
+    __device__ static int value_at(int t, int d) {
         return 16 * DP + piece(t / 8 * 16 + d / kRows, t % 8 * kUnit + d % kRows / 2);
     }
     __device__ static int value_power(int t, int block) { return value_powers(block) + t; }
@@ -99,6 +97,7 @@ struct KvRows {                      // [b][row][head][dim], the channels contig
 struct KvTokens {                    // the tokens a write or read takes
     const int *table, *first, *counts;
     int table_pages, B, n;
+    int records;                     // of a sequence and head that n tokens may reach into
 };
 
 struct AttendArgs {

@@ -7,28 +7,45 @@
 
 namespace wf {
 
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
+typedef float f2 __attribute__((ext_vector_type(2)));
+
 constexpr int kKvThreads = 256;
 
 // ---- kernels ----------------------------------------------------------------
 
-// The head's record that holds token `pos`, or null with the reason in the
-// error word.
+// What a workgroup writes or reads: one record of one head, the tokens of it
+// that the call takes.  Records are the cache's, not the call's, so that a wave
+// takes tokens whose bytes lie together whatever the call's first token is.
+struct KvWork {
+    uint8_t* record;                 // null: not to be touched, `reason` says why
+    int b, head, reason;
+    long long i0;                    // the call's token at the record's start, which may be before its first
+    int count;
+};
+
 template <int DP>
-__device__ __forceinline__ uint8_t* kv_record(const KvCache& c, const int* table, int table_pages, int b, int head, int pos) {
-    const int at = pos >> c.page_shift;
-    if (pos < 0 || at >= table_pages) {
-        atomicOr(c.err, kErrKvRange);
-        return nullptr;
+__device__ __forceinline__ KvWork kv_work(const KvCache& c, const KvTokens& a) {
+    const int head = blockIdx.x % c.heads, rec = blockIdx.x / c.heads % a.records, b = blockIdx.x / c.heads / a.records;
+    const int first = a.first[b], count = a.counts ? min(a.counts[b], a.n) : a.n;
+    const long long at = (long long)(first >> 5) + rec;            // the record's place in the sequence
+    KvWork w{nullptr, b, head, 0, at * kKvTile - first, count};
+    const int per_page = c.page_shift - 5;
+    if (at < 0 || at >> per_page >= a.table_pages) {
+        w.reason = kErrKvRange;
+        return w;
     }
-    const int page = table[(size_t)b * table_pages + at];
+    const int page = a.table[(size_t)b * a.table_pages + (at >> per_page)];
     if (page < 0 || page >= c.pages) {
-        atomicOr(c.err, kErrKvPage);
-        return nullptr;
+        w.reason = kErrKvPage;
+        return w;
     }
-    return c.pool + (size_t)page * c.page_bytes() + (size_t)head * c.head_bytes() +
-           (size_t)((pos & ((1 << c.page_shift) - 1)) / kKvTile) * KvLayout<DP>::kRecord;
+    w.record = c.pool + (size_t)page * c.page_bytes() + (size_t)head * c.head_bytes() +
+               (size_t)(at & ((1 << per_page) - 1)) * KvLayout<DP>::kRecord;
+    return w;
 }
 
+// Eight channels of which m exist.
 template <class T>
 __device__ __forceinline__ void load8(const T* p, int m, float (&x)[8]) {
     if (m >= 8) {
@@ -38,135 +55,177 @@ __device__ __forceinline__ void load8(const T* p, int m, float (&x)[8]) {
         for (int e = 0; e < 8; ++e) x[e] = (float)t[e];
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = e < m ? (float)p[e] : 0.0f;
+        for (int e = 0; e < 8; ++e) x[e] = 0.0f;
     }
 }
 
-template <class T>
-__device__ __forceinline__ void store8(T* p, int m, const float (&x)[8]) {
-    if (m >= 8) {
-        T t[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) t[e] = (T)x[e];
-        __builtin_memcpy(p, t, sizeof t);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < m) p[e] = (T)x[e];
-    }
+// The power byte of a block whose largest magnitude has the bits `top`, and
+// the factor 2^-e.  The smallest power with 6 * 2^e >= top: 6 is 1.5 * 2^2, so
+// e is top's exponent less 2, and one more where its mantissa is above 1.5.
+__device__ __forceinline__ unsigned kv_power(unsigned top, float& inv) {
+    const bool nan = top >= 0x7f800000u;
+    int e = (int)((top + 0x3fffffu) >> 23) - 129;
+    e = e < -kKvMaxPower ? -kKvMaxPower : (e > kKvMaxPower ? kKvMaxPower : e);
+    inv = nan ? 0.0f : __builtin_bit_cast(float, (unsigned)(127 - e) << 23);   // exact: a power of two
+    return nan ? kKvNan : e + 127;
 }
 
-// One lane quantises eight channels; four lanes share a block.
+// Eight channels as 4-bit codes, rounded to the nearest (a tie to the even
+// code) and cut off at 6; a block that is not finite holds zeros.
+__device__ __forceinline__ unsigned kv_code(const float (&x)[8], float inv) {
+    unsigned code = 0;
+    if (inv == 0.0f) return code;
+    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[0] * inv, x[1] * inv, 1.0f, 0);
+    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[2] * inv, x[3] * inv, 1.0f, 1);
+    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[4] * inv, x[5] * inv, 1.0f, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[6] * inv, x[7] * inv, 1.0f, 3);
+}
+
+// Lanes take eight channels of a token each, the token's first, then the next
+// token: four lanes share a block.  Bound by memory.
 template <int DP, class T>
 __global__ __launch_bounds__(kKvThreads) void k_kv_write(KvCache c, KvRows k, KvRows v, KvTokens a) {
     using L = KvLayout<DP>;
-    constexpr int W = DP / 8;
-    const long long id = (long long)blockIdx.x * kKvThreads + threadIdx.x;
-    const int w = id % W;
-    const long long r = id / W;
-    const int head = r % c.heads;
-    const long long bi = r / c.heads;
-    const int i = bi % a.n, b = bi / a.n;
-    const bool value = blockIdx.y;
-    uint8_t* base = nullptr;
-    int pos = 0;
-    float x[8] = {};
-    if (b < a.B && i < (a.counts ? a.counts[b] : a.n)) {
-        pos = a.first[b] + i;
-        base = kv_record<DP>(c, a.table, a.table_pages, b, head, pos);
-        const KvRows& s = value ? v : k;
-        load8((const T*)s.p + b * s.sb + i * s.sr + head * s.sh + w * 8, c.dim - w * 8, x);
-    }
-    // the bits of |x| order as the values do; a NaN's lie above infinity's
-    unsigned top = 0;
+    constexpr int W = DP / 8, N = kKvTile * W / kKvThreads;        // words of a token; a lane's tokens
+    const KvWork o = kv_work<DP>(c, a);
+    const int w = threadIdx.x % W;
+    float x[2][N][8];
+    bool on[N];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, __builtin_bit_cast(unsigned, x[e]) & 0x7fffffffu);
-    top = max(top, (unsigned)__shfl_xor((int)top, 1));
-    top = max(top, (unsigned)__shfl_xor((int)top, 2));
-    if (!base) return;
-    // the smallest power with 6 * 2^e >= top: 6 is 1.5 * 2^2, so e is top's
-    // exponent less 2, and one more where its mantissa is above 1.5
-    const bool nan = top >= 0x7f800000u;
-    int e = (int)((top + 0x3fffffu) >> 23) - 129;
-    e = nan || e < -kKvMaxPower ? -kKvMaxPower : (e > kKvMaxPower ? kKvMaxPower : e);
-    const float inv = __builtin_bit_cast(float, (unsigned)(127 - e) << 23);   // exact: a power of two
-    unsigned code = 0;
-    if (!nan) {
-        // round to nearest even, saturating at 6
-        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[0] * inv, x[1] * inv, 1.0f, 0);
-        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[2] * inv, x[3] * inv, 1.0f, 1);
-        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[4] * inv, x[5] * inv, 1.0f, 2);
-        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[6] * inv, x[7] * inv, 1.0f, 3);
-    }
-    const int t = pos & (kKvTile - 1);
-    const uint8_t power = nan ? kKvNan : e + 127;
-    if (!value) {
-        *(unsigned*)(base + L::key_word(t, w)) = code;
-        if (w % 4 == 0) base[L::key_power(t, w / 4)] = power;
-    } else {
-        uint8_t* at = base + L::value_word(t, w);
-        if constexpr (L::kRows == 4) {
-            *(uint16_t*)at = (uint16_t)code;
-            *(uint16_t*)(at + 16) = (uint16_t)(code >> 16);
+    for (int j = 0; j < N; ++j) {
+        const int t = (j * kKvThreads + threadIdx.x) / W;
+        const long long i = o.i0 + t;
+        on[j] = i >= 0 && i < o.count;
+        if (on[j] && o.record) {
+            load8((const T*)k.p + o.b * k.sb + i * k.sr + o.head * k.sh + w * 8, c.dim - w * 8, x[0][j]);
+            load8((const T*)v.p + o.b * v.sb + i * v.sr + o.head * v.sh + w * 8, c.dim - w * 8, x[1][j]);
         } else {
-            *(unsigned*)at = code;
+            if (on[j]) atomicOr(c.err, o.reason);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[0][j][e] = x[1][j][e] = 0.0f;
         }
-        if (w % 4 == 0) base[L::value_power(t, w / 4)] = power;
+    }
+    if (!o.record) return;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int t = (j * kKvThreads + threadIdx.x) / W;
+        unsigned code[2], power[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            // the bits of |x| order as the values do; a NaN's lie above infinity's
+            unsigned top = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = max(top, __builtin_bit_cast(unsigned, x[s][j][e]) & 0x7fffffffu);
+            top = max(top, (unsigned)__shfl_xor((int)top, 1));
+            top = max(top, (unsigned)__shfl_xor((int)top, 2));
+            float inv;
+            power[s] = kv_power(top, inv);
+            code[s] = kv_code(x[s][j], inv);
+        }
+        uint8_t* at = o.record + L::value_at(t, w * 8);
+        if constexpr (L::kRows == 4) {
+            // a word is half of two lanes' runs: where the token beside this
+            // one is written too, the pair of lanes swaps halves
+            const unsigned other = (unsigned)__shfl_xor((int)code[1], W);
+            const bool both = __shfl_xor((int)on[j], W);
+            if (on[j]) {
+                if (both) {
+                    if (t % 2 == 0) *(unsigned*)at = (code[1] & 0xffff) | other << 16;
+                    else *(unsigned*)(at + 14) = other >> 16 | (code[1] & 0xffff0000u);
+                } else {
+                    *(uint16_t*)at = (uint16_t)code[1];
+                    *(uint16_t*)(at + 16) = (uint16_t)(code[1] >> 16);
+                }
+            }
+        } else if (on[j]) {
+            *(unsigned*)at = code[1];
+        }
+        if (on[j]) {
+            *(unsigned*)(o.record + L::key_at(t, w * 8)) = code[0];
+            if (w % 4 == 0) {
+                o.record[L::key_power(t, w / 4)] = (uint8_t)power[0];
+                o.record[L::value_power(t, w / 4)] = (uint8_t)power[1];
+            }
+        }
     }
 }
 
-// One lane reads eight channels back.  Tokens past a sequence's count, and
-// those that the table does not reach, are zeros.
-template <int DP, class T>
+// The same tokens read back, 16 bytes of a token a lane.  Those past a
+// sequence's count, and those that the table does not reach, are zeros.
+// STREAM, for aligned rows: stores that pass the caches by.  Written through
+// them, 8 heads of 128 in bf16 take 9.7 us for 4096 tokens and 37.6 for 32768;
+// past them 5.6 and 27.1, more than what a kernel that reads the result next
+// then loses (1.2 and 4.4 us).
+template <int DP, class T, bool STREAM>
 __global__ __launch_bounds__(kKvThreads) void k_kv_read(KvCache c, KvRows k, KvRows v, KvTokens a) {
     using L = KvLayout<DP>;
-    typedef float f2 __attribute__((ext_vector_type(2)));
-    constexpr int W = DP / 8;
-    const long long id = (long long)blockIdx.x * kKvThreads + threadIdx.x;
-    const int w = id % W;
-    const long long r = id / W;
-    const int head = r % c.heads;
-    const long long bi = r / c.heads;
-    const int i = bi % a.n, b = bi / a.n;
-    const bool value = blockIdx.y;
-    if (b >= a.B || w * 8 >= c.dim) return;
-    const KvRows& s = value ? v : k;
-    T* out = (T*)s.p + b * s.sb + i * s.sr + head * s.sh + w * 8;
-    float x[8] = {};
-    if (i < (a.counts ? a.counts[b] : a.n)) {
-        const int pos = a.first[b] + i, t = pos & (kKvTile - 1);
-        const uint8_t* base = kv_record<DP>(c, a.table, a.table_pages, b, head, pos);
-        if (base) {
-            unsigned code, power;
-            if (!value) {
-                code = *(const unsigned*)(base + L::key_word(t, w));
-                power = base[L::key_power(t, w / 4)];
-            } else {
-                const uint8_t* at = base + L::value_word(t, w);
-                if constexpr (L::kRows == 4) code = *(const uint16_t*)at | (unsigned)*(const uint16_t*)(at + 16) << 16;
-                else code = *(const unsigned*)at;
-                power = base[L::value_power(t, w / 4)];
-            }
-            const float scale = __builtin_bit_cast(float, power << 23);   // 255: the conversion gives NaN
-#define WF_PAIR(j)                                                                    \
-    {                                                                                 \
-        const f2 y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, scale, j);        \
-        x[2 * j] = y[0];                                                              \
-        x[2 * j + 1] = y[1];                                                          \
+    constexpr int C = 16 / sizeof(T), W = DP / C, N = kKvTile * W / kKvThreads;   // channels of a lane; lanes of a token
+    const KvWork o = kv_work<DP>(c, a);
+    const int d = threadIdx.x % W * C;
+    unsigned code[2][N], power[2][N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int t = (j * kKvThreads + threadIdx.x) / W;
+        const long long i = o.i0 + t;
+        code[0][j] = code[1][j] = power[0][j] = power[1][j] = 0;
+        if (i < 0 || i >= o.count) continue;
+        if (!o.record) {
+            atomicOr(c.err, o.reason);
+            continue;
+        }
+        const uint8_t *kp = o.record + L::key_at(t, d), *vp = o.record + L::value_at(t, d);
+        if constexpr (C == 4) {
+            code[0][j] = *(const uint16_t*)kp;
+            code[1][j] = *(const uint16_t*)vp;
+        } else {
+            code[0][j] = *(const unsigned*)kp;
+            if constexpr (L::kRows == 4) code[1][j] = *(const uint16_t*)vp | (unsigned)*(const uint16_t*)(vp + 16) << 16;
+            else code[1][j] = *(const unsigned*)vp;
+        }
+        power[0][j] = o.record[L::key_power(t, d / kKvBlock)];
+        power[1][j] = o.record[L::value_power(t, d / kKvBlock)];
     }
-            WF_PAIR(0) WF_PAIR(1) WF_PAIR(2) WF_PAIR(3)
-#undef WF_PAIR
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int t = (j * kKvThreads + threadIdx.x) / W;
+        const long long i = o.i0 + t;
+        if (i < 0 || i >= a.n || d >= c.dim) continue;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const KvRows& r = s ? v : k;
+            const float scale = __builtin_bit_cast(float, power[s][j] << 23);   // 255: the conversion gives NaN
+            T x[C];
+            auto two = [&](int e, const f2& y) {
+                x[e] = (T)y[0];
+                x[e + 1] = (T)y[1];
+            };
+            two(0, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[s][j], scale, 0));
+            two(2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[s][j], scale, 1));
+            if constexpr (C == 8) {
+                two(4, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[s][j], scale, 2));
+                two(6, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[s][j], scale, 3));
+            }
+            T* out = (T*)r.p + o.b * r.sb + i * r.sr + o.head * r.sh + d;
+            if constexpr (STREAM) {
+                u4 u;
+                __builtin_memcpy(&u, x, 16);
+                __builtin_nontemporal_store(u, (u4*)out);
+            } else {
+                __builtin_memcpy(out, x, 16);
+            }
         }
     }
-    store8(out, c.dim - w * 8, x);
 }
 
 template <int DP, class T>
 static void launch_kv(bool write, const KvCache& c, const KvRows& k, const KvRows& v, const KvTokens& a, hipStream_t st) {
-    const long long lanes = (long long)a.B * a.n * c.heads * (DP / 8);
-    const dim3 grid((unsigned)((lanes + kKvThreads - 1) / kKvThreads), 2);
+    const dim3 grid((unsigned)((long long)a.B * a.records * c.heads));
+    auto aligned = [](const KvRows& r) {
+        return ((uintptr_t)r.p | (uintptr_t)((r.sb | r.sr | r.sh) * sizeof(T))) % 16 == 0;
+    };
     if (write) hipLaunchKernelGGL((k_kv_write<DP, T>), grid, dim3(kKvThreads), 0, st, c, k, v, a);
-    else hipLaunchKernelGGL((k_kv_read<DP, T>), grid, dim3(kKvThreads), 0, st, c, k, v, a);
+    else if (aligned(k) && aligned(v)) hipLaunchKernelGGL((k_kv_read<DP, T, true>), grid, dim3(kKvThreads), 0, st, c, k, v, a);
+    else hipLaunchKernelGGL((k_kv_read<DP, T, false>), grid, dim3(kKvThreads), 0, st, c, k, v, a);
 }
 
 template <class T>
@@ -217,9 +276,10 @@ static int kv_tokens(const Cache* c, int precision, int B, int n, const int32_t*
     if (precision != WF_FP32 && precision != WF_BF16) return fail(WF_E_INVALID, "unknown precision");
     if (B < 0 || n < 0 || table_pages < 0) return fail(WF_E_INVALID, "B, n and table_pages must not be negative");
     if (B && n && (!table || !first)) return fail(WF_E_INVALID, "table or first is NULL");
-    if ((long long)B * n * c->c.heads * (c->c.dp / 8) / kKvThreads >= 0x7fffffffLL)
-        return fail(WF_E_UNSUPPORTED, "more than 2^39 channels in one call");
-    *out = {table, first, counts, table_pages, B, n};
+    // records that n tokens may reach into, wherever the first one lies
+    const long long records = ((long long)n + 2 * (kKvTile - 1)) / kKvTile;
+    if (B * records * c->c.heads >= 0x7fffffffLL) return fail(WF_E_UNSUPPORTED, "more than 2^31 records in one call");
+    *out = {table, first, counts, table_pages, B, n, (int)records};
     return WF_OK;
 }
 
