@@ -92,26 +92,35 @@ __device__ __forceinline__ unsigned pair_of(unsigned w, float power) {
 
 // A tile of 32 tokens of one head as a lane holds it.
 template <int DP>
-struct AtTile {
-    unsigned k[DP / 16], v[DP / 16], kp, vp[2];
+struct AtKeys {
+    unsigned w[DP / 16], power;
+};
+template <int DP>
+struct AtValues {
+    unsigned w[DP / 16], power[2];
 };
 
 template <int DP>
-__device__ __forceinline__ void load_tile(AtTile<DP>& t, const uint8_t* record, int lane) {
+__device__ __forceinline__ void load_keys(AtKeys<DP>& k, const uint8_t* record, int lane) {
     using L = KvLayout<DP>;
 #pragma unroll
-    for (int n = 0; n < L::kLane; n += 16) {
-        __builtin_memcpy(t.k + n / 4, __builtin_assume_aligned(record + L::piece(lane, n), 16), 16);
-        __builtin_memcpy(t.v + n / 4, __builtin_assume_aligned(record + 16 * DP + L::piece(lane, n), 16), 16);
-    }
+    for (int n = 0; n < L::kLane; n += 16) __builtin_memcpy(k.w + n / 4, __builtin_assume_aligned(record + L::piece(lane, n), 16), 16);
     if constexpr (L::kPowers == 2) {
         uint16_t p;
         __builtin_memcpy(&p, __builtin_assume_aligned(record + L::key_lane_powers(lane), 2), 2);
-        t.kp = p;
+        k.power = p;
     } else {
-        __builtin_memcpy(&t.kp, __builtin_assume_aligned(record + L::key_lane_powers(lane), 4), 4);
+        __builtin_memcpy(&k.power, __builtin_assume_aligned(record + L::key_lane_powers(lane), 4), 4);
     }
-    __builtin_memcpy(t.vp, __builtin_assume_aligned(record + L::value_powers((lane & 15) * L::kRows / kKvBlock) + 8 * (lane >> 4), 8), 8);
+}
+
+template <int DP>
+__device__ __forceinline__ void load_values(AtValues<DP>& v, const uint8_t* record, int lane) {
+    using L = KvLayout<DP>;
+    __builtin_memcpy(v.power, __builtin_assume_aligned(record + L::value_powers((lane & 15) * L::kRows / kKvBlock) + 8 * (lane >> 4), 8), 8);
+#pragma unroll
+    for (int n = 0; n < L::kLane; n += 16)
+        __builtin_memcpy(v.w + n / 4, __builtin_assume_aligned(record + 16 * DP + L::piece(lane, n), 16), 16);
 }
 
 // Byte N of a word as a power of two.
@@ -122,16 +131,16 @@ __device__ __forceinline__ float power_at(unsigned w) {
 
 // The operand of half A of the keys, channels from 8 KK of each quarter.
 template <int DP, int A, int KK>
-__device__ __forceinline__ b8 key_frag(const AtTile<DP>& t) {
+__device__ __forceinline__ b8 key_frag(const AtKeys<DP>& t) {
     constexpr int kPerLane = KvLayout<DP>::kPowers / 2;    // powers of a half in a lane
-    const unsigned w = t.k[A * (DP / 32) + KK];
-    const float power = power_at<A * kPerLane + KK * kPerLane / (DP / 32)>(t.kp);
+    const unsigned w = t.w[A * (DP / 32) + KK];
+    const float power = power_at<A * kPerLane + KK * kPerLane / (DP / 32)>(t.power);
     u4 r = {pair_of<0>(w, power), pair_of<1>(w, power), pair_of<2>(w, power), pair_of<3>(w, power)};
     return __builtin_bit_cast(b8, r);
 }
 
 template <int DP, int NT, int NQ, int A, int KK = 0>
-__device__ __forceinline__ void add_scores(const AtTile<DP>& x, const b8 (&q)[NT][DP / 32][NQ], f4 (&s)[NT][2]) {
+__device__ __forceinline__ void add_scores(const AtKeys<DP>& x, const b8 (&q)[NT][DP / 32][NQ], f4 (&s)[NT][2]) {
     if constexpr (KK < DP / 32) {
         const b8 f = key_frag<DP, A, KK>(x);
 #pragma unroll
@@ -200,7 +209,7 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, int b, int head, 
 
 // Waves of a SIMD that the registers are shared out for.
 template <int DP, class T, int NT>
-constexpr int kAtWgs = NT * DP * (int)sizeof(T) <= 128 * 2 ? 3 : (NT * DP * (int)sizeof(T) <= 256 * 2 ? 2 : 1);
+constexpr int kAtWgs = NT == 1 && DP * (int)sizeof(T) <= 256 ? 4 : NT * DP * (int)sizeof(T) <= 128 * 2 ? 3 : (NT * DP * (int)sizeof(T) <= 256 * 2 ? 2 : 1);
 
 // One workgroup: 16 NT rows of a sequence's key head, and a share of its
 // tokens.
@@ -267,7 +276,9 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
     const size_t page_bytes = a.c.page_bytes();
 
     f4 o[NT][ND], l[NT], bad[NT];
-    float m[NT], sub[NT], raise[NT];       // maximum; what is subtracted; where it is raised
+    // the row's maximum so far, and the score that raises it (none: 0 and
+    // -infinity)
+    float sub[NT], raise[NT];
     b8 ones;
 #pragma unroll
     for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.0f;
@@ -282,15 +293,20 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
 #pragma unroll
             for (int r = 0; r < ND; ++r) o[t][r] = f4{0, 0, 0, 0};
             l[t] = bad[t] = f4{0, 0, 0, 0};
-            m[t] = raise[t] = -INFINITY;
+            raise[t] = -INFINITY;
             sub[t] = 0.0f;
         }
-        AtTile<DP> buf[2];
-        u2 allow[2][NT];                   // the mask's bytes of the lane's tokens
-        auto load = [&](AtTile<DP>& x, u2 (&allow)[NT], int tile, int page) {
-            const bool there = page >= 0 && page < a.c.pages;
-            if constexpr (MASK) {
-                const int at = tile * kKvTile + 8 * g;
+        const int tile0 = t0 + wave;
+        if (tile0 < t1) {
+            AtKeys<DP> keys;
+            AtValues<DP> values;
+            u2 allow[NT];                  // the mask's bytes of the lane's tokens
+            auto page_of = [&](int tile) { return table[min(tile, t1 - 1) >> in_page]; };
+            auto record_of = [&](int tile, int page) {
+                return pool + (size_t)page * page_bytes + (size_t)(min(tile, t1 - 1) & ((1 << in_page) - 1)) * L::kRecord;
+            };
+            auto load_mask = [&](int tile) {
+                const int at = min(tile, t1 - 1) * kKvTile + 8 * g;
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     if (at + 8 <= a.max_visible) {
@@ -301,114 +317,110 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
                         allow[t] = __builtin_bit_cast(u2, x);
                     }
                 }
-            }
-            load_tile<DP>(x, pool + (size_t)(there ? page : 0) * page_bytes + (size_t)(tile & ((1 << in_page) - 1)) * L::kRecord, lane);
-            return there;
-        };
-        auto take = [&](const AtTile<DP>& x, const u2 (&allow)[NT], int tile) {
-            f4 s[NT][2];
+            };
+            // a page outside the pool: its tokens are left out (another page's
+            // are loaded in their place)
+            auto inside = [&](int page) { return page >= 0 && page < a.c.pages; };
+            int page = page_of(tile0), next = page_of(tile0 + NW);
+            bool there = inside(page), missing = !there;
+            const uint8_t* record = record_of(tile0, there ? page : 0);
+            load_keys(keys, record, lane);
+            if constexpr (MASK) load_mask(tile0);
+            load_values(values, record, lane);
+            // Keys and values of the next tile are loaded as soon as this
+            // one's are used up, and the page of the one after it.  Past the
+            // end it is the last tile again, so that the loads in flight are
+            // the same on every path.
+            for (int tile = tile0; tile < t1; tile += NW) {
+                const bool next_there = inside(next);
+                record = record_of(tile + NW, next_there ? next : 0);
+                next = page_of(tile + 2 * NW);
+                f4 s[NT][2];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = f4{0, 0, 0, 0};
-            add_scores<DP, NT, NQ, 0>(x, q, s);
-            add_scores<DP, NT, NQ, 1>(x, q, s);
-            const int at = tile * kKvTile + 8 * g;         // the lane's first token
-            const bool edge = MASK || care || (tile + 1) * kKvTile > least;   // some row may not see all of it
-            unsigned sees[NT];
-            if (edge) {
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const int left = see[t] - at;
-                    sees[t] = 0;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        bool on = e < left;
-                        if constexpr (MASK) on = on && (allow[t][e / 4] >> 8 * (e % 4) & 0xff);
-                        sees[t] |= (unsigned)on << e;
-                        s[t][e / 4][e % 4] = on ? s[t][e / 4][e % 4] : -INFINITY;
-                    }
-                }
-            }
-            float power[8] = {power_at<0>(x.vp[0]), power_at<1>(x.vp[0]), power_at<2>(x.vp[0]), power_at<3>(x.vp[0]),
-                              power_at<0>(x.vp[1]), power_at<1>(x.vp[1]), power_at<2>(x.vp[1]), power_at<3>(x.vp[1])};
-            if (edge) {
-                // past the last token that any row sees, a page holds anything
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e >= most - at) power[e] = 1.0f;
-                if (care) {
-                    unsigned spoilt = 0;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (power[e] == INFINITY) {
-                            spoilt |= 1u << e;
-                            power[e] = 1.0f;
-                        }
-                    b8 is;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) is[e] = (__bf16)(float)(spoilt >> e & 1);
+                for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = f4{0, 0, 0, 0};
+                add_scores<DP, NT, NQ, 0>(keys, q, s);
+                add_scores<DP, NT, NQ, 1>(keys, q, s);
+                load_keys(keys, record, lane);
+                const int at = tile * kKvTile + 8 * g;         // the lane's first token
+                const bool edge = MASK || care || !there || (tile + 1) * kKvTile > least;   // some row may not see all of it
+                unsigned sees[NT];
+                if (edge) {
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
-                        b8 on;
+                        const int left = there ? see[t] - at : 0;
+                        sees[t] = 0;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) on[e] = (__bf16)(float)(sees[t] >> e & 1);
-                        bad[t] = mfma(is, on, bad[t]);
+                        for (int e = 0; e < 8; ++e) {
+                            bool on = e < left;
+                            if constexpr (MASK) on = on && (allow[t][e / 4] >> 8 * (e % 4) & 0xff);
+                            sees[t] |= (unsigned)on << e;
+                            s[t][e / 4][e % 4] = on ? s[t][e / 4][e % 4] : -INFINITY;
+                        }
                     }
                 }
-            }
-            b8 p[NT][NP];
+                if constexpr (MASK) load_mask(tile + NW);
+                float power[8] = {power_at<0>(values.power[0]), power_at<1>(values.power[0]), power_at<2>(values.power[0]), power_at<3>(values.power[0]),
+                                  power_at<0>(values.power[1]), power_at<1>(values.power[1]), power_at<2>(values.power[1]), power_at<3>(values.power[1])};
+                if (edge) {
+                    // past the last token that any row sees, a page holds anything
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                // NaN where a score is: the row's maximum then stays as it is,
-                // and its outputs become NaN through the exponent
-                float top = s[t][0][0];
+                    for (int e = 0; e < 8; ++e)
+                        if (!there || e >= most - at) power[e] = 1.0f;
+                    if (care) {
+                        unsigned spoilt = 0;
 #pragma unroll
-                for (int e = 1; e < 8; ++e) top = __builtin_elementwise_maximum(top, s[t][e / 4][e % 4]);
-                top *= a.scale_log2;
-                if (__any(top > raise[t])) {
-                    top = fmaxf(top, __shfl_xor(top, 16));
-                    top = fmaxf(top, __shfl_xor(top, 32));
-                    const float next = fmaxf(m[t], top), by = m[t] == -INFINITY ? 0.0f : exp2f(m[t] - next);
-                    if (next != -INFINITY) {
-                        m[t] = sub[t] = next;
-                        raise[t] = next + kAtSlack;
+                        for (int e = 0; e < 8; ++e)
+                            if (power[e] == INFINITY) {
+                                spoilt |= 1u << e;
+                                power[e] = 1.0f;
+                            }
+                        b8 is;
 #pragma unroll
-                        for (int r = 0; r < ND; ++r) o[t][r] *= by;
-                        l[t] *= by;
+                        for (int e = 0; e < 8; ++e) is[e] = (__bf16)(float)(spoilt >> e & 1);
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            b8 on;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) on[e] = (__bf16)(float)(sees[t] >> e & 1);
+                            bad[t] = mfma(is, on, bad[t]);
+                        }
                     }
                 }
-                float w[8];
+                b8 p[NT][NP];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e / 4][e % 4], a.scale_log2, -sub[t]));
-                parts<NP>(w, p[t]);
+                for (int t = 0; t < NT; ++t) {
+                    // NaN where a score is: the row's maximum then stays as it is,
+                    // and its outputs become NaN through the exponent
+                    float top = s[t][0][0];
 #pragma unroll
-                for (int n = NP - 1; n >= 0; --n) l[t] = mfma(ones, p[t][n], l[t]);
-            }
-            add_values<DP, NT, NP>(x.v, power, p, o);
-        };
-        // The next tile is loaded while one is worked on, and the page of the
-        // one after it; past the end it is the last one again, so that the
-        // loads in flight are the same on every path.
-        int tile = t0 + wave;
-        if (tile < t1) {
-            auto page_of = [&](int t) { return table[min(t, t1 - 1) >> in_page]; };
-            int page = page_of(tile);
-            bool there[2];
-            there[0] = load(buf[0], allow[0], tile, page);
-            page = page_of(tile + NW);
-            while (tile < t1) {
+                    for (int e = 1; e < 8; ++e) top = __builtin_elementwise_maximum(top, s[t][e / 4][e % 4]);
+                    top *= a.scale_log2;
+                    if (__any(top > raise[t])) {
+                        top = fmaxf(top, __shfl_xor(top, 16));
+                        top = fmaxf(top, __shfl_xor(top, 32));
+                        const bool none = raise[t] == -INFINITY;
+                        const float most = none ? top : fmaxf(sub[t], top), by = none ? 0.0f : exp2f(sub[t] - most);
+                        if (most != -INFINITY) {
+                            sub[t] = most;
+                            raise[t] = most + kAtSlack;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    there[1 - h] = load(buf[1 - h], allow[1 - h], min(tile + NW, t1 - 1), page);
-                    page = page_of(tile + 2 * NW);
-                    if (!there[h]) {
-                        if (lane == 0) atomicOr(a.c.err, kErrKvPage);
-                    } else {
-                        take(buf[h], allow[h], tile);
+                            for (int r = 0; r < ND; ++r) o[t][r] *= by;
+                            l[t] *= by;
+                        }
                     }
-                    tile += NW;
-                    if (tile >= t1) break;
+                    float w[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e / 4][e % 4], a.scale_log2, -sub[t]));
+                    parts<NP>(w, p[t]);
+#pragma unroll
+                    for (int n = NP - 1; n >= 0; --n) l[t] = mfma(ones, p[t][n], l[t]);
                 }
+                add_values<DP, NT, NP>(values.w, power, p, o);
+                load_values(values, record, lane);
+                there = next_there;
+                missing |= !there;
             }
+            if (missing && lane == 0) atomicOr(a.c.err, kErrKvPage);
         }
         if (care) break;
         bool nan = false;
@@ -438,7 +450,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
     for (int t = 0; t < NT; ++t) {
         if (t) __syncthreads();
         if (lane < 16) {
-            sm[wave][lane] = m[t];
+            sm[wave][lane] = raise[t] == -INFINITY ? -INFINITY : sub[t];
             sl[wave][lane] = l[t][0];
         }
 #pragma unroll
@@ -562,7 +574,7 @@ void attend_plan(AttendArgs& a, int precision) {
     const int nt = row_tiles(a, precision), rows = a.n * a.group, waves = nt == 1 && (precision == WF_BF16 || a.c.dp < 256) ? 8 : 4;
     const long long groups = (long long)a.B * a.c.heads * ((rows + 16 * nt - 1) / (16 * nt));
     // workgroups that keep the chip busy, with at least four tiles for each wave
-    long long s = (kAtTarget + groups - 1) / groups;
+    long long s = kAtTarget / groups;
     const long long by_len = a.max_visible / (4 * waves * kKvTile);
     s = s < by_len ? s : by_len;
     const long long by_room = kAttendWorkRows / (groups * 16 * nt);

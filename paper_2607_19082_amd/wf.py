@@ -66,8 +66,8 @@ class CacheDesc(ctypes.Structure):
                 ("page", ctypes.c_int32)]
 
 
-class Rows(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_int64 * 3)]
+# wf_rows: a pointer and three strides, as four words
+Rows = ctypes.c_int64 * 4
 
 
 class Out(ctypes.Structure):
@@ -107,11 +107,10 @@ def lib():
         L.wf_synthesis.argtypes = [P, P, P, P]
         L.wf_xform_destroy.argtypes = [P]
         i32 = ctypes.c_int32
-        rows = ctypes.POINTER(Rows)
         L.wf_cache_plan.argtypes = [ctypes.POINTER(CacheDesc), ctypes.POINTER(ctypes.c_void_p)]
-        L.wf_cache_write.argtypes = [P, i32, rows, rows, i32, i32, P, i32, P, P, P]
-        L.wf_cache_read.argtypes = [P, i32, rows, rows, i32, i32, P, i32, P, P, P]
-        L.wf_cache_attend.argtypes = [P, i32, rows, rows, i32, i32, i32, P, i32, P, P, P, i32, ctypes.c_float, P]
+        L.wf_cache_write.argtypes = [P, i32, P, P, i32, i32, P, i32, P, P, P]
+        L.wf_cache_read.argtypes = [P, i32, P, P, i32, i32, P, i32, P, P, P]
+        L.wf_cache_attend.argtypes = [P, i32, P, P, i32, i32, i32, P, i32, P, P, P, i32, ctypes.c_float, P]
         L.wf_cache_sync.argtypes = [P, P]
         L.wf_cache_destroy.argtypes = [P]
         L.wf_plan_trace.argtypes = [P, P, ctypes.c_int64, P, P]
@@ -468,10 +467,17 @@ class Cache:
     what a kernel found wrong."""
 
     def __init__(self, heads, dim, pages, page=64):
+        import torch
         h = ctypes.c_void_p()
         _check(lib().wf_cache_plan(ctypes.byref(CacheDesc(heads, dim, pages, page)), ctypes.byref(h)))
         self._h = h
         self.heads, self.dim, self.pages, self.page = heads, dim, pages, page
+        # a serving step makes several short calls: what they look up is kept
+        self._lib, self._torch = lib(), torch
+        self._precision = {torch.float32: 0, torch.bfloat16: 1}
+        # the handle of a device's current stream, without a Stream object
+        self._current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
     def close(self):
         if getattr(self, "_h", None):
@@ -486,35 +492,38 @@ class Cache:
 
     @staticmethod
     def _rows(t, shape, dtype, name):
-        if not t.is_cuda or t.dtype != dtype or t.shape != shape or (t.stride(3) != 1 and t.numel()):
-            raise ValueError(f"{name}: expected a {dtype} CUDA tensor {tuple(shape)} with contiguous channels, got "
-                             f"{t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
         st = t.stride()
-        return Rows(t.data_ptr(), (st[0], st[1], st[2]))
+        if not t.is_cuda or t.dtype != dtype or t.shape != shape or (st[3] != 1 and t.numel()):
+            raise ValueError(f"{name}: expected a {dtype} CUDA tensor {tuple(shape)} with contiguous channels, got "
+                             f"{t.dtype} {tuple(t.shape)}, strides {st}, on {t.device}")
+        return Rows(t.data_ptr(), st[0], st[1], st[2])
 
-    @staticmethod
-    def _ints(t, shape, name):
-        import torch
-        if not t.is_cuda or t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
+    def _ints(self, t, shape, name):
+        if not t.is_cuda or t.dtype != self._torch.int32 or t.shape != shape or not t.is_contiguous():
             raise ValueError(f"{name}: expected a contiguous int32 CUDA tensor {tuple(shape)}, got {t.dtype} "
                              f"{tuple(t.shape)} on {t.device}")
         return t.data_ptr()
 
-    @staticmethod
-    def _precision(dtype):
-        import torch
-        if dtype == torch.bfloat16:
-            return 1
-        if dtype == torch.float32:
-            return 0
-        raise ValueError(f"expected torch.float32 or torch.bfloat16, got {dtype}")
+    def _type(self, dtype):
+        precision = self._precision.get(dtype)
+        if precision is None:
+            raise ValueError(f"expected torch.float32 or torch.bfloat16, got {dtype}")
+        return precision
 
-    def _tokens(self, B, n, table, first, counts):
+    def _table(self, table, B):
         if table.dim() != 2:
             raise ValueError(f"table: expected two dimensions, got {tuple(table.shape)}")
         pages = table.shape[1]
-        return (self._ints(table, (B, pages), "table"), pages, self._ints(first, (B,), "first"),
-                None if counts is None else self._ints(counts, (B,), "counts"))
+        return self._ints(table, (B, pages), "table"), pages
+
+    def _empty(self, shape, dtype, device, stream):
+        t = self._torch.empty(shape, dtype=dtype, device=device)
+        if stream is not None:          # allocated on the current stream, used on another
+            t.record_stream(stream)
+        return t
+
+    def _stream(self, stream, device):
+        return self._current(device.index) if stream is None else stream.cuda_stream
 
     def write(self, k, v, table, first, counts=None, stream=None):
         """Quantise k and v [B][n][heads][dim] into the cache: token i of
@@ -522,27 +531,33 @@ class Cache:
         if k.dim() != 4:
             raise ValueError(f"k: expected four dimensions, got {tuple(k.shape)}")
         B, n = k.shape[:2]
-        shape = (B, n, self.heads, self.dim)
-        kr, vr = self._rows(k, shape, k.dtype, "k"), self._rows(v, shape, k.dtype, "v")
-        p_table, pages, p_first, p_counts = self._tokens(B, n, table, first, counts)
-        _check(lib().wf_cache_write(self._h, self._precision(k.dtype), kr, vr, B, n, p_table, pages, p_first, p_counts,
-                                    _stream_handle(stream)))
+        shape, dtype = (B, n, self.heads, self.dim), k.dtype
+        p_table, pages = self._table(table, B)
+        rc = self._lib.wf_cache_write(
+            self._h, self._type(dtype), self._rows(k, shape, dtype, "k"), self._rows(v, shape, dtype, "v"), B, n, p_table,
+            pages, self._ints(first, (B,), "first"), None if counts is None else self._ints(counts, (B,), "counts"),
+            self._stream(stream, k.device))
+        if rc:
+            _check(rc)
 
     def read(self, table, first, n, counts=None, dtype=None, out=None, stream=None):
         """Tokens first[b] .. first[b] + n - 1 of every sequence as the values
         they stand for: (k, v) [B][n][heads][dim] of `dtype` (default fp32), or
         written to the pair `out`.  Tokens past counts[b] are zeros."""
-        import torch
         B = table.shape[0]
+        p_table, pages = self._table(table, B)
         shape = (B, n, self.heads, self.dim)
         if out is None:
-            dtype = torch.float32 if dtype is None else dtype
-            out = (torch.empty(shape, dtype=dtype, device=table.device), torch.empty(shape, dtype=dtype, device=table.device))
+            dtype = self._torch.float32 if dtype is None else dtype
+            out = (self._empty(shape, dtype, table.device, stream), self._empty(shape, dtype, table.device, stream))
         k, v = out
-        kr, vr = self._rows(k, shape, k.dtype, "k"), self._rows(v, shape, k.dtype, "v")
-        p_table, pages, p_first, p_counts = self._tokens(B, n, table, first, counts)
-        _check(lib().wf_cache_read(self._h, self._precision(k.dtype), kr, vr, B, n, p_table, pages, p_first, p_counts,
-                                   _stream_handle(stream)))
+        dtype = k.dtype
+        rc = self._lib.wf_cache_read(
+            self._h, self._type(dtype), self._rows(k, shape, dtype, "k"), self._rows(v, shape, dtype, "v"), B, n, p_table,
+            pages, self._ints(first, (B,), "first"), None if counts is None else self._ints(counts, (B,), "counts"),
+            self._stream(stream, table.device))
+        if rc:
+            _check(rc)
         return k, v
 
     def attend(self, q, table, visible, scale=None, mask=None, max_visible=None, out=None, stream=None):
@@ -553,30 +568,28 @@ class Cache:
         the cache's heads; scale defaults to dim ** -0.5.  max_visible bounds
         visible (default: the mask's width, or all that the table holds; a
         tighter bound makes a better launch)."""
-        import torch
         if q.dim() != 4:
             raise ValueError(f"q: expected four dimensions, got {tuple(q.shape)}")
         B, n, hq = q.shape[:3]
-        shape = (B, n, hq, self.dim)
-        if table.dim() != 2:
-            raise ValueError(f"table: expected two dimensions, got {tuple(table.shape)}")
-        pages = table.shape[1]
+        shape, dtype = (B, n, hq, self.dim), q.dtype
+        p_table, pages = self._table(table, B)
         if max_visible is None:
             max_visible = pages * self.page if mask is None else mask.shape[-1]
         if out is None:
-            out = torch.empty(shape, dtype=q.dtype, device=q.device)
-        qr, outr = self._rows(q, shape, q.dtype, "q"), self._rows(out, shape, q.dtype, "out")
+            out = self._empty(shape, dtype, q.device, stream)
         p_mask = strides = None
         if mask is not None:
-            if not mask.is_cuda or mask.dtype != torch.bool or mask.shape != (B, n, max_visible) or \
+            if not mask.is_cuda or mask.dtype != self._torch.bool or mask.shape != (B, n, max_visible) or \
                     (max_visible > 1 and mask.stride(2) != 1):
                 raise ValueError(f"mask: expected a bool CUDA tensor {(B, n, max_visible)} with contiguous tokens, got "
                                  f"{mask.dtype} {tuple(mask.shape)}, strides {mask.stride()}")
             p_mask, strides = mask.data_ptr(), (ctypes.c_int64 * 2)(mask.stride(0), mask.stride(1))
-        _check(lib().wf_cache_attend(self._h, self._precision(q.dtype), qr, outr, B, n, hq,
-                                     self._ints(table, (B, pages), "table"), pages, self._ints(visible, (B, n), "visible"),
-                                     p_mask, strides, max_visible, self.dim ** -0.5 if scale is None else scale,
-                                     _stream_handle(stream)))
+        rc = self._lib.wf_cache_attend(
+            self._h, self._type(dtype), self._rows(q, shape, dtype, "q"), self._rows(out, shape, dtype, "out"), B, n, hq,
+            p_table, pages, self._ints(visible, (B, n), "visible"), p_mask, strides, max_visible,
+            self.dim ** -0.5 if scale is None else scale, self._stream(stream, q.device))
+        if rc:
+            _check(rc)
         return out
 
     def sync(self, stream=None):
