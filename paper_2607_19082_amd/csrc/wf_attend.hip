@@ -104,23 +104,26 @@ template <int DP>
 __device__ __forceinline__ void load_keys(AtKeys<DP>& k, const uint8_t* record, int lane) {
     using L = KvLayout<DP>;
 #pragma unroll
-    for (int n = 0; n < L::kLane; n += 16) __builtin_memcpy(k.w + n / 4, __builtin_assume_aligned(record + L::piece(lane, n), 16), 16);
+    for (int n = 0; n < L::kLane; n += 16)
+        __builtin_memcpy(k.w + n / 4, __builtin_assume_aligned(record + L::piece(0, n) + lane * 16u, 16), 16);
+    const uint8_t* powers = record + 32 * DP + (unsigned)(L::key_lane_powers(lane) - 32 * DP);
     if constexpr (L::kPowers == 2) {
         uint16_t p;
-        __builtin_memcpy(&p, __builtin_assume_aligned(record + L::key_lane_powers(lane), 2), 2);
+        __builtin_memcpy(&p, __builtin_assume_aligned(powers, 2), 2);
         k.power = p;
     } else {
-        __builtin_memcpy(&k.power, __builtin_assume_aligned(record + L::key_lane_powers(lane), 4), 4);
+        __builtin_memcpy(&k.power, __builtin_assume_aligned(powers, 4), 4);
     }
 }
 
 template <int DP>
 __device__ __forceinline__ void load_values(AtValues<DP>& v, const uint8_t* record, int lane) {
     using L = KvLayout<DP>;
-    __builtin_memcpy(v.power, __builtin_assume_aligned(record + L::value_powers((lane & 15) * L::kRows / kKvBlock) + 8 * (lane >> 4), 8), 8);
+    const unsigned powers = L::value_powers((lane & 15) * L::kRows / kKvBlock) - L::value_powers(0) + 8 * (lane >> 4);
+    __builtin_memcpy(v.power, __builtin_assume_aligned(record + L::value_powers(0) + powers, 8), 8);
 #pragma unroll
     for (int n = 0; n < L::kLane; n += 16)
-        __builtin_memcpy(v.w + n / 4, __builtin_assume_aligned(record + 16 * DP + L::piece(lane, n), 16), 16);
+        __builtin_memcpy(v.w + n / 4, __builtin_assume_aligned(record + 16 * DP + L::piece(0, n) + lane * 16u, 16), 16);
 }
 
 // Byte N of a word as a power of two.
@@ -326,12 +329,14 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
             const uint8_t* record = record_of(tile0, there ? page : 0);
             load_keys(keys, record, lane);
             if constexpr (MASK) load_mask(tile0);
-            load_values(values, record, lane);
-            // Keys and values of the next tile are loaded as soon as this
-            // one's are used up, and the page of the one after it.  Past the
-            // end it is the last tile again, so that the loads in flight are
-            // the same on every path.
+            // The next tile's keys are loaded as soon as this one's are used
+            // up, its values then, and the page of the one after it.  Past
+            // the end it is the last tile again, so that the loads in flight
+            // are the same on every path.
             for (int tile = tile0; tile < t1; tile += NW) {
+                load_values(values, record, lane);
+                // the loads go out before the wait for the keys
+                __builtin_amdgcn_sched_barrier(0);
                 const bool next_there = inside(next);
                 record = record_of(tile + NW, next_there ? next : 0);
                 next = page_of(tile + 2 * NW);
@@ -416,7 +421,6 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
                     for (int n = NP - 1; n >= 0; --n) l[t] = mfma(ones, p[t][n], l[t]);
                 }
                 add_values<DP, NT, NP>(values.w, power, p, o);
-                load_values(values, record, lane);
                 there = next_there;
                 missing |= !there;
             }
