@@ -39,6 +39,7 @@ typedef unsigned u2 __attribute__((ext_vector_type(2)));
 typedef const int __attribute__((address_space(4))) * SharedInts;
 
 constexpr int kAtTarget = 256;      // workgroups that a call is split into
+constexpr int kAtMaxSplits = 256;
 constexpr int kAtJoin = 256;        // threads of the kernel that joins the splits
 // waves of a workgroup
 template <int DP, class T, int NT>
@@ -84,6 +85,27 @@ __device__ __forceinline__ void parts(const float (&x)[8], b8 (&p)[N]) {
     }
 }
 
+// The part of eight values that a lane's column holds: what `skip` (a lane's
+// pairs (-1, 0), (0, -1) or zeros for each part before its own) leaves.
+template <int N>
+__device__ __forceinline__ b8 part_of(const float (&x)[8], const unsigned (&skip)[N][2]) {
+    b8 p;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        f2 r = {x[e], x[e + 1]};
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const b2 h = __builtin_convertvector(r, b2);
+            r[0] = __builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(b2, skip[n][0]), r[0], false);
+            r[1] = __builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(b2, skip[n][1]), r[1], false);
+        }
+        const b2 h = __builtin_convertvector(r, b2);
+        p[e] = h[0];
+        p[e + 1] = h[1];
+    }
+    return p;
+}
+
 // Two 4-bit values of byte J of w, times the power, as a pair of bf16.
 template <int J>
 __device__ __forceinline__ unsigned pair_of(unsigned w, float power) {
@@ -126,11 +148,14 @@ __device__ __forceinline__ void load_values(AtValues<DP>& v, const uint8_t* reco
         __builtin_memcpy(v.w + n / 4, __builtin_assume_aligned(record + 16 * DP + L::piece(0, n) + lane * 16u, 16), 16);
 }
 
-// Byte N of a word as a power of two.
+// Byte N of a word as the exponent of a scale.  The bits beside it are the
+// word's others: a conversion reads the exponent alone.
 template <int N>
 __device__ __forceinline__ float power_at(unsigned w) {
-    return __builtin_bit_cast(float, (N == 0 ? w << 23 : (N == 1 ? w << 15 : (N == 2 ? w << 7 : w >> 1))) & 0x7f800000u);
+    return __builtin_bit_cast(float, N == 0 ? w << 23 : (N == 1 ? w << 15 : (N == 2 ? w << 7 : w >> 1)));
 }
+
+__device__ __forceinline__ bool power_is_nan(float p) { return (~__builtin_bit_cast(unsigned, p) & 0x7f800000u) == 0; }
 
 // The operand of half A of the keys, channels from 8 KK of each quarter.
 template <int DP, int A, int KK>
@@ -210,15 +235,21 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, int b, int head, 
     __builtin_memcpy((T*)a.o.p + b * a.o.sb + i * a.o.sr + h * a.o.sh + d, out, sizeof out);
 }
 
+// PACK: with few rows a column tile holds every row once for each part of its
+// probabilities, so that one product takes all parts; the columns of a row are
+// summed at the end.  Rows that then fit a tile:
+template <class T>
+constexpr int kAtPackRows = sizeof(T) == 2 ? 8 : 4;
+
 // Waves of a SIMD that the registers are shared out for.
 template <int DP, class T, int NT>
 constexpr int kAtWgs = NT == 1 && DP * (int)sizeof(T) <= 256 ? 4 : NT * DP * (int)sizeof(T) <= 128 * 2 ? 3 : (NT * DP * (int)sizeof(T) <= 256 * 2 ? 2 : 1);
 
 // One workgroup: 16 NT rows of a sequence's key head, and a share of its
 // tokens.
-template <int DP, class T, int NT, bool MASK>
+template <int DP, class T, int NT, bool MASK, bool PACK>
 __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) void k_attend(AttendArgs a) {
-    constexpr int NW = kAtWaves<DP, T, NT>, NQ = AtParts<T>::kQ, NP = AtParts<T>::kP, NK = DP / 32, ND = DP / 16;
+    constexpr int NW = kAtWaves<DP, T, NT>, NQ = AtParts<T>::kQ, NP = PACK ? 1 : AtParts<T>::kP, NK = DP / 32, ND = DP / 16;
     using L = KvLayout<DP>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int rows = a.n * a.group, nrt = (rows + 16 * NT - 1) / (16 * NT);
@@ -232,7 +263,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
     const uint8_t* mask[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const int row = rt * 16 * NT + t * 16 + col;
+        const int row = rt * 16 * NT + t * 16 + (PACK ? col % kAtPackRows<T> : col);
         const bool on = row < rows;
         const int i = on ? row / a.group : 0, h = head * a.group + (on ? row % a.group : 0);
         int s = on ? a.visible[(size_t)b * a.n + i] : 0;
@@ -278,6 +309,13 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
     const uint8_t* pool = a.c.pool + (size_t)head * a.c.head_bytes();
     const size_t page_bytes = a.c.page_bytes();
 
+    constexpr int kSkip = AtParts<T>::kP - 1;
+    unsigned skip[kSkip][2];
+#pragma unroll
+    for (int n = 0; n < kSkip; ++n) {
+        skip[n][0] = PACK && col / kAtPackRows<T> > n ? 0x0000bf80u : 0u;
+        skip[n][1] = PACK && col / kAtPackRows<T> > n ? 0xbf800000u : 0u;
+    }
     f4 o[NT][ND], l[NT], bad[NT];
     // the row's maximum so far, and the score that raises it (none: 0 and
     // -infinity)
@@ -375,7 +413,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
                         unsigned spoilt = 0;
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
-                            if (power[e] == INFINITY) {
+                            if (power_is_nan(power[e])) {
                                 spoilt |= 1u << e;
                                 power[e] = 1.0f;
                             }
@@ -416,7 +454,8 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
                     float w[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e / 4][e % 4], a.scale_log2, -sub[t]));
-                    parts<NP>(w, p[t]);
+                    if constexpr (PACK) p[t][0] = part_of<kSkip>(w, skip);
+                    else parts<NP>(w, p[t]);
 #pragma unroll
                     for (int n = NP - 1; n >= 0; --n) l[t] = mfma(ones, p[t][n], l[t]);
                 }
@@ -476,6 +515,13 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
                 by[w] = at_weight(sm[w][c], sl[w][c], most);
                 sum += by[w] * sl[w][c];
             }
+            // the parts of a row (a lane's column and those beside it)
+            if constexpr (PACK) {
+                float all = sum;
+#pragma unroll
+                for (int n = 1; n <= kSkip; ++n) all += __shfl(sum, (c + n * kAtPackRows<T>) % 16);
+                sum = all;
+            }
             const float scale = a.splits > 1 ? 1.0f : (sum == 0.0f ? 0.0f : 1.0f / sum);
 #pragma unroll
             for (int w = 0; w < NW; ++w) sm[w][c] = by[w] * scale;
@@ -488,11 +534,14 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
             f8 v = {};
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
-                f8 y;
-                __builtin_memcpy(&y, __builtin_assume_aligned(&lds[(w * 16 + c) * kPitch + d], 16), sizeof y);
                 const float by = sm[w][c];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += by * y[e];
+                for (int n = 0; n <= (PACK ? kSkip : 0); ++n) {
+                    f8 y;
+                    __builtin_memcpy(&y, __builtin_assume_aligned(&lds[(w * 16 + c + n * kAtPackRows<T>) * kPitch + d], 16), sizeof y);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] += by * y[e];
+                }
             }
             if (a.splits == 1) {
                 if (d < a.c.dim) write_row<T>(a, b, head, row0 + t * 16 + c, d, v);
@@ -509,50 +558,69 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
 }
 
 // Joins the splits of one row: eight channels a lane, the splits dealt to
-// groups of lanes that join at the end.
+// groups of lanes.  The first wave turns the splits' maxima and sums into
+// weights while the partial results are on their way.
 template <int DP, class T>
 __global__ __launch_bounds__(kAtJoin) void k_attend_join(AttendArgs a, int tile_rows) {
-    constexpr int W = DP / 8, G = kAtJoin / W;
-    __shared__ float so[G][DP], sm[G], sl[G];
-    const int rows = a.n * a.group, row = blockIdx.x % rows, bh = blockIdx.x / rows, g = threadIdx.x / W, d = threadIdx.x % W * 8;
-    const int nrt = (rows + tile_rows - 1) / tile_rows;
+    constexpr int W = DP / 8, G = kAtJoin / W, K = kAtMaxSplits / 64, Y = 4;
+    __shared__ float weight[kAtMaxSplits], so[kAtJoin / 64][DP];
+    const unsigned rows = a.n * a.group, row = blockIdx.x % rows, bh = blockIdx.x / rows;
+    const int g = threadIdx.x / W, d = threadIdx.x % W * 8, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const unsigned nrt = (rows + tile_rows - 1) / tile_rows;
     const size_t first = ((size_t)bh * nrt + (nrt - 1 - row / tile_rows)) * a.splits * tile_rows + row % tile_rows;
-    float top = -INFINITY, sum = 0.0f;
-    f8 v = {};
-    auto add = [&](float m, float l, const f8& x) {
-        if (m == -INFINITY && l == 0.0f) return;         // it saw no token
-        const float next = fmaxf(top, m), old = top == next ? 1.0f : exp2f(top - next), by = m == next ? 1.0f : exp2f(m - next);
-        sum = old * sum + by * l;
+    const float* po = a.part_o + first * DP + d;
+    f8 y[Y];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = old * v[e] + by * x[e];
-        top = next;
-    };
-    for (int s = g; s < a.splits; s += 4 * G) {
-        f2 z[4];
-        f8 y[4];
+    for (int j = 0; j < Y; ++j)
+        __builtin_memcpy(&y[j], __builtin_assume_aligned(po + (size_t)min(g + j * G, a.splits - 1) * tile_rows * DP, 16), 32);
+    if (wave == 0) {
+        f2 z[K];
+        float most = -INFINITY, sum = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const size_t at = first + (size_t)min(s + j * G, a.splits - 1) * tile_rows;
-            __builtin_memcpy(&z[j], __builtin_assume_aligned(a.part_ml + at * 2, 8), 8);
-            __builtin_memcpy(&y[j], __builtin_assume_aligned(a.part_o + at * DP + d, 16), 32);
+        for (int k = 0; k < K; ++k) {
+            z[k] = f2{-INFINITY, 0.0f};
+            if (k * 64 + lane < a.splits)
+                __builtin_memcpy(&z[k], __builtin_assume_aligned(a.part_ml + (first + (size_t)(k * 64 + lane) * tile_rows) * 2, 8), 8);
+            most = fmaxf(most, z[k][0]);
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (s + j * G < a.splits) add(z[j][0], z[j][1], y[j]);
-    }
-    __builtin_memcpy(__builtin_assume_aligned(&so[g][d], 16), &v, 32);
-    if (d == 0) {
-        sm[g] = top;
-        sl[g] = sum;
+        for (int x = 1; x < 64; x <<= 1) most = fmaxf(most, __shfl_xor(most, x));
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            z[k][0] = at_weight(z[k][0], z[k][1], most);
+            sum += z[k][0] * z[k][1];
+        }
+#pragma unroll
+        for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
+        const float scale = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+        for (int k = 0; k < K; ++k) weight[k * 64 + lane] = z[k][0] * scale;
     }
     __syncthreads();
-    if (g || d >= a.c.dim) return;
-    for (int j = 1; j < min(G, a.splits); ++j) {
-        f8 y;
-        __builtin_memcpy(&y, __builtin_assume_aligned(&so[j][d], 16), 32);
-        add(sm[j], sl[j], y);
+    f8 v = {};
+    for (int s = g; s < a.splits; s += Y * G) {
+#pragma unroll
+        for (int j = 0; j < Y; ++j)
+            if (s + j * G < a.splits) v += weight[s + j * G] * y[j];
+        if (s + Y * G < a.splits)
+#pragma unroll
+            for (int j = 0; j < Y; ++j)
+                __builtin_memcpy(&y[j], __builtin_assume_aligned(po + (size_t)min(s + (Y + j) * G, a.splits - 1) * tile_rows * DP, 16), 32);
     }
-    v *= sum == 0.0f ? 0.0f : 1.0f / sum;
+    // the groups of a wave, then the waves
+#pragma unroll
+    for (int x = W; x < 64; x <<= 1)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += __shfl_xor(v[e], x);
+    if (lane < W) __builtin_memcpy(__builtin_assume_aligned(&so[wave][d], 16), &v, 32);
+    __syncthreads();
+    if (threadIdx.x >= W || d >= a.c.dim) return;
+#pragma unroll
+    for (int w = 1; w < kAtJoin / 64; ++w) {
+        f8 z;
+        __builtin_memcpy(&z, __builtin_assume_aligned(&so[w][d], 16), 32);
+        v += z;
+    }
     write_row<T>(a, bh / a.c.heads, bh % a.c.heads, row, d, v);
 }
 
@@ -583,7 +651,13 @@ void attend_plan(AttendArgs& a, int precision) {
     s = s < by_len ? s : by_len;
     const long long by_room = kAttendWorkRows / (groups * 16 * nt);
     s = s < by_room ? s : by_room;
+    s = s < kAtMaxSplits ? s : kAtMaxSplits;
     a.splits = s < 2 ? 1 : (int)s;
+}
+
+template <int DP, class T, int NT>
+static void join(const AttendArgs& a, hipStream_t st) {
+    hipLaunchKernelGGL((k_attend_join<DP, T>), dim3((unsigned)(a.B * a.c.heads * a.n * a.group)), dim3(kAtJoin), 0, st, a, 16 * NT);
 }
 
 template <int DP, class T, int NT>
@@ -592,10 +666,18 @@ static void launch_nt(const AttendArgs& a, hipStream_t st) {
     const long long groups = (long long)a.B * a.c.heads * ((rows + 16 * NT - 1) / (16 * NT));
     constexpr int kThreads = 64 * kAtWaves<DP, T, NT>;
     const dim3 grid((unsigned)(groups * a.splits));
-    if (a.mask) hipLaunchKernelGGL((k_attend<DP, T, NT, true>), grid, dim3(kThreads), 0, st, a);
-    else hipLaunchKernelGGL((k_attend<DP, T, NT, false>), grid, dim3(kThreads), 0, st, a);
-    if (a.splits > 1)
-        hipLaunchKernelGGL((k_attend_join<DP, T>), dim3((unsigned)(a.B * a.c.heads * rows)), dim3(kAtJoin), 0, st, a, 16 * NT);
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, a); };
+    if constexpr (NT == 1) {
+        if (rows <= kAtPackRows<T>) {
+            if (a.mask) launch(k_attend<DP, T, NT, true, true>);
+            else launch(k_attend<DP, T, NT, false, true>);
+            if (a.splits > 1) join<DP, T, NT>(a, st);
+            return;
+        }
+    }
+    if (a.mask) launch(k_attend<DP, T, NT, true, false>);
+    else launch(k_attend<DP, T, NT, false, false>);
+    if (a.splits > 1) join<DP, T, NT>(a, st);
 }
 
 template <int DP, class T>
