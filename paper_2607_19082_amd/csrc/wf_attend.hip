@@ -23,6 +23,7 @@
 // few rows the tokens are also split over workgroups, and a second kernel
 // joins their results.
 #include <cmath>
+#include <type_traits>
 
 #include "wf_cache.h"
 
@@ -30,6 +31,8 @@ namespace wf {
 
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef float f8 __attribute__((ext_vector_type(8)));
 typedef float f2 __attribute__((ext_vector_type(2)));
 typedef __bf16 b2 __attribute__((ext_vector_type(2)));
@@ -47,19 +50,46 @@ constexpr int kAtWaves = NT == 1 && DP * sizeof(T) < 1024 ? 8 : 4;
 // a row's maximum is raised only when a score passes it by this much (in
 // powers of two): its probabilities then stay below 2^8
 constexpr float kAtSlack = 8.0f;
+// Probabilities are held times 2^7, so that half precision takes them up to
+// that (2^15) and loses none above 2^-32 of the row's largest; the sums that
+// divide them are too.
+constexpr float kAtLift = 7.0f;
+// Power bytes 109 to 140 (2^-18 to 2^13): all values that they scale are exact
+// in half precision.
+constexpr unsigned kAtWindow = 0x6d6d6d6du;
 
+// parts of queries (bf16), of probabilities in half precision, and in bf16
 template <class T>
 struct AtParts;
 template <>
 struct AtParts<__bf16> {
-    static constexpr int kQ = 1, kP = 2;
+    static constexpr int kQ = 1, kH = 0, kP = 2;
 };
 template <>
 struct AtParts<float> {
-    static constexpr int kQ = 3, kP = 3;
+    static constexpr int kQ = 3, kH = 2, kP = 3;
 };
 
 __device__ __forceinline__ f4 mfma(b8 a, b8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+__device__ __forceinline__ f4 mfma(h8 a, h8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// Eight values as N parts in half precision, the largest first.
+template <int N>
+__device__ __forceinline__ void parts(const float (&x)[8], h8 (&p)[N]) {
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        f2 r = {x[e], x[e + 1]};
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const h2 h = __builtin_convertvector(r, h2);
+            p[n][e] = h[0];
+            p[n][e + 1] = h[1];
+            r[0] = __builtin_fmaf((float)h[0], -1.0f, r[0]);
+            r[1] = __builtin_fmaf((float)h[1], -1.0f, r[1]);
+        }
+    }
+}
 
 // Eight values as N bf16 parts, the largest first.  What a part leaves is one
 // dot product: r - 1 * part + 0 * its neighbour, exact.  The pairs (-1, 0) and
@@ -85,31 +115,12 @@ __device__ __forceinline__ void parts(const float (&x)[8], b8 (&p)[N]) {
     }
 }
 
-// The part of eight values that a lane's column holds: what `skip` (a lane's
-// pairs (-1, 0), (0, -1) or zeros for each part before its own) leaves.
-template <int N>
-__device__ __forceinline__ b8 part_of(const float (&x)[8], const unsigned (&skip)[N][2]) {
-    b8 p;
-#pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-        f2 r = {x[e], x[e + 1]};
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const b2 h = __builtin_convertvector(r, b2);
-            r[0] = __builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(b2, skip[n][0]), r[0], false);
-            r[1] = __builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(b2, skip[n][1]), r[1], false);
-        }
-        const b2 h = __builtin_convertvector(r, b2);
-        p[e] = h[0];
-        p[e + 1] = h[1];
-    }
-    return p;
-}
-
-// Two 4-bit values of byte J of w, times the power, as a pair of bf16.
-template <int J>
+// Two 4-bit values of byte J of w, times the power, as a pair of the type that
+// V8 is a vector of.
+template <int J, class V8>
 __device__ __forceinline__ unsigned pair_of(unsigned w, float power) {
-    return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, J));
+    if constexpr (std::is_same<V8, h8>::value) return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, power, J));
+    else return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, J));
 }
 
 // A tile of 32 tokens of one head as a lane holds it.
@@ -163,7 +174,7 @@ __device__ __forceinline__ b8 key_frag(const AtKeys<DP>& t) {
     constexpr int kPerLane = KvLayout<DP>::kPowers / 2;    // powers of a half in a lane
     const unsigned w = t.w[A * (DP / 32) + KK];
     const float power = power_at<A * kPerLane + KK * kPerLane / (DP / 32)>(t.power);
-    u4 r = {pair_of<0>(w, power), pair_of<1>(w, power), pair_of<2>(w, power), pair_of<3>(w, power)};
+    u4 r = {pair_of<0, b8>(w, power), pair_of<1, b8>(w, power), pair_of<2, b8>(w, power), pair_of<3, b8>(w, power)};
     return __builtin_bit_cast(b8, r);
 }
 
@@ -181,34 +192,34 @@ __device__ __forceinline__ void add_scores(const AtKeys<DP>& x, const b8 (&q)[NT
 
 // Tiles 2 B and 2 B + 1 of the values as operands: rows are channels kRows i +
 // 2 B (+ 1), k the lane's eight tokens.
-template <int DP, int B>
-__device__ __forceinline__ void value_frags(const unsigned (&v)[DP / 16], const float (&power)[8], b8 (&f)[2]) {
+template <int DP, int B, class V8>
+__device__ __forceinline__ void value_frags(const unsigned (&v)[DP / 16], const float (&power)[8], V8 (&f)[2]) {
     u4 lo, hi;
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         unsigned x, y;
         if constexpr (DP == 64) {                 // a word holds two tokens
-            x = pair_of<B>(v[p], power[2 * p]);
-            y = pair_of<B + 2>(v[p], power[2 * p + 1]);
+            x = pair_of<B, V8>(v[p], power[2 * p]);
+            y = pair_of<B + 2, V8>(v[p], power[2 * p + 1]);
         } else if constexpr (DP == 128) {
-            x = pair_of<B>(v[2 * p], power[2 * p]);
-            y = pair_of<B>(v[2 * p + 1], power[2 * p + 1]);
+            x = pair_of<B, V8>(v[2 * p], power[2 * p]);
+            y = pair_of<B, V8>(v[2 * p + 1], power[2 * p + 1]);
         } else {                                  // two words a token
-            x = pair_of<B % 4>(v[4 * p + B / 4], power[2 * p]);
-            y = pair_of<B % 4>(v[4 * p + 2 + B / 4], power[2 * p + 1]);
+            x = pair_of<B % 4, V8>(v[4 * p + B / 4], power[2 * p]);
+            y = pair_of<B % 4, V8>(v[4 * p + 2 + B / 4], power[2 * p + 1]);
         }
         lo[p] = __builtin_amdgcn_perm(y, x, 0x05040100);
         hi[p] = __builtin_amdgcn_perm(y, x, 0x07060302);
     }
-    f[0] = __builtin_bit_cast(b8, lo);
-    f[1] = __builtin_bit_cast(b8, hi);
+    f[0] = __builtin_bit_cast(V8, lo);
+    f[1] = __builtin_bit_cast(V8, hi);
 }
 
-template <int DP, int NT, int NP, int B = 0>
-__device__ __forceinline__ void add_values(const unsigned (&v)[DP / 16], const float (&power)[8], const b8 (&p)[NT][NP],
+template <int DP, int NT, int NP, int B = 0, class V8>
+__device__ __forceinline__ void add_values(const unsigned (&v)[DP / 16], const float (&power)[8], const V8 (&p)[NT][NP],
                                            f4 (&o)[NT][DP / 16]) {
     if constexpr (B < DP / 32) {
-        b8 f[2];
+        V8 f[2];
         value_frags<DP, B>(v, power, f);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
@@ -218,6 +229,30 @@ __device__ __forceinline__ void add_values(const unsigned (&v)[DP / 16], const f
                 for (int t = 0; t < NT; ++t) o[t][2 * B + s] = mfma(f[s], p[t][m], o[t][2 * B + s]);
         add_values<DP, NT, NP, B + 1>(v, power, p, o);
     }
+}
+
+// Eight bits as ones and zeros.
+__device__ __forceinline__ b8 bits(unsigned x) {
+    b8 r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = (__bf16)(float)(x >> e & 1);
+    return r;
+}
+
+// The tile's probabilities into their sums and, times its values, the outputs.
+template <int DP, int NT, int N, class V8>
+__device__ __forceinline__ void add_products(const unsigned (&v)[DP / 16], const float (&power)[8], const float (&w)[NT][8], f4 (&l)[NT],
+                                             f4 (&o)[NT][DP / 16]) {
+    V8 p[NT][N], ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = 1.0f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        parts<N>(w[t], p[t]);
+#pragma unroll
+        for (int n = N - 1; n >= 0; --n) l[t] = mfma(ones, p[t][n], l[t]);
+    }
+    add_values<DP, NT, N>(v, power, p, o);
 }
 
 // Weight of a partial result with maximum m and sum l; 0 where it saw no token.
@@ -235,21 +270,15 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, int b, int head, 
     __builtin_memcpy((T*)a.o.p + b * a.o.sb + i * a.o.sr + h * a.o.sh + d, out, sizeof out);
 }
 
-// PACK: with few rows a column tile holds every row once for each part of its
-// probabilities, so that one product takes all parts; the columns of a row are
-// summed at the end.  Rows that then fit a tile:
-template <class T>
-constexpr int kAtPackRows = sizeof(T) == 2 ? 8 : 4;
-
 // Waves of a SIMD that the registers are shared out for.
 template <int DP, class T, int NT>
 constexpr int kAtWgs = NT == 1 && DP * (int)sizeof(T) <= 256 ? 4 : NT * DP * (int)sizeof(T) <= 128 * 2 ? 3 : (NT * DP * (int)sizeof(T) <= 256 * 2 ? 2 : 1);
 
 // One workgroup: 16 NT rows of a sequence's key head, and a share of its
 // tokens.
-template <int DP, class T, int NT, bool MASK, bool PACK>
+template <int DP, class T, int NT, bool MASK>
 __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) void k_attend(AttendArgs a) {
-    constexpr int NW = kAtWaves<DP, T, NT>, NQ = AtParts<T>::kQ, NP = PACK ? 1 : AtParts<T>::kP, NK = DP / 32, ND = DP / 16;
+    constexpr int NW = kAtWaves<DP, T, NT>, NQ = AtParts<T>::kQ, NP = AtParts<T>::kP, NH = AtParts<T>::kH, NK = DP / 32, ND = DP / 16;
     using L = KvLayout<DP>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int rows = a.n * a.group, nrt = (rows + 16 * NT - 1) / (16 * NT);
@@ -263,7 +292,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
     const uint8_t* mask[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const int row = rt * 16 * NT + t * 16 + (PACK ? col % kAtPackRows<T> : col);
+        const int row = rt * 16 * NT + t * 16 + col;
         const bool on = row < rows;
         const int i = on ? row / a.group : 0, h = head * a.group + (on ? row % a.group : 0);
         int s = on ? a.visible[(size_t)b * a.n + i] : 0;
@@ -309,26 +338,21 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
     const uint8_t* pool = a.c.pool + (size_t)head * a.c.head_bytes();
     const size_t page_bytes = a.c.page_bytes();
 
-    constexpr int kSkip = AtParts<T>::kP - 1;
-    unsigned skip[kSkip][2];
-#pragma unroll
-    for (int n = 0; n < kSkip; ++n) {
-        skip[n][0] = PACK && col / kAtPackRows<T> > n ? 0x0000bf80u : 0u;
-        skip[n][1] = PACK && col / kAtPackRows<T> > n ? 0xbf800000u : 0u;
-    }
     f4 o[NT][ND], l[NT], bad[NT];
     // the row's maximum so far, and the score that raises it (none: 0 and
     // -infinity)
     float sub[NT], raise[NT];
-    b8 ones;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.0f;
 
-    // The pass is repeated with care where a value that is not a number
-    // reached an output: it may stand at a token that only other rows see, and
-    // 0 times it is not 0.  With care such blocks are taken as zeros, and a
+    // One pass over the wave's tiles; false where it has to be made again with
+    // care: where a value lies outside half precision's window (fp32 calls), or
+    // one that is not a number reached an output (bf16 calls; it may stand at a
+    // token that only other rows see, and 0 times it is not 0).  The careful
+    // pass takes values in bf16, and blocks that are not finite as zeros; a
     // count of those that each row sees says which channels they spoil.
-    for (int care = 0; care < 2; ++care) {
+    auto pass = [&](auto careful) {
+        constexpr bool kCareful = decltype(careful)::value, kHalf = !kCareful && sizeof(T) == 4;
+        using V8 = typename std::conditional<kHalf, h8, b8>::type;
+        bool fits = true;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -371,7 +395,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
             // up, its values then, and the page of the one after it.  Past
             // the end it is the last tile again, so that the loads in flight
             // are the same on every path.
-            for (int tile = tile0; tile < t1; tile += NW) {
+            for (int tile = tile0; tile < t1 && fits; tile += NW) {
                 load_values(values, record, lane);
                 // the loads go out before the wait for the keys
                 __builtin_amdgcn_sched_barrier(0);
@@ -385,8 +409,10 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
                 add_scores<DP, NT, NQ, 1>(keys, q, s);
                 load_keys(keys, record, lane);
                 const int at = tile * kKvTile + 8 * g;         // the lane's first token
-                const bool edge = MASK || care || !there || (tile + 1) * kKvTile > least;   // some row may not see all of it
-                unsigned sees[NT];
+                const bool edge = MASK || !there || (tile + 1) * kKvTile > least;   // some row may not see all of it
+                unsigned sees[NT];                     // the lane's tokens that its row sees
+#pragma unroll
+                for (int t = 0; t < NT; ++t) sees[t] = 0xff;
                 if (edge) {
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
@@ -402,34 +428,28 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
                     }
                 }
                 if constexpr (MASK) load_mask(tile + NW);
-                float power[8] = {power_at<0>(values.power[0]), power_at<1>(values.power[0]), power_at<2>(values.power[0]), power_at<3>(values.power[0]),
-                                  power_at<0>(values.power[1]), power_at<1>(values.power[1]), power_at<2>(values.power[1]), power_at<3>(values.power[1])};
                 if (edge) {
                     // past the last token that any row sees, a page holds anything
+                    const int n = max(0, min(8, there ? most - at : 0));
+                    const uint64_t in = n == 8 ? ~0ull : (1ull << 8 * n) - 1;
+                    values.power[0] = (values.power[0] & (unsigned)in) | (0x7f7f7f7fu & ~(unsigned)in);
+                    values.power[1] = (values.power[1] & (unsigned)(in >> 32)) | (0x7f7f7f7fu & ~(unsigned)(in >> 32));
+                }
+                if constexpr (kHalf) fits = !__any(((values.power[0] - kAtWindow) | (values.power[1] - kAtWindow)) & 0xe0e0e0e0u);
+                float power[8] = {power_at<0>(values.power[0]), power_at<1>(values.power[0]), power_at<2>(values.power[0]), power_at<3>(values.power[0]),
+                                  power_at<0>(values.power[1]), power_at<1>(values.power[1]), power_at<2>(values.power[1]), power_at<3>(values.power[1])};
+                if constexpr (kCareful) {
+                    unsigned spoilt = 0;
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        if (!there || e >= most - at) power[e] = 1.0f;
-                    if (care) {
-                        unsigned spoilt = 0;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (power_is_nan(power[e])) {
-                                spoilt |= 1u << e;
-                                power[e] = 1.0f;
-                            }
-                        b8 is;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) is[e] = (__bf16)(float)(spoilt >> e & 1);
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) {
-                            b8 on;
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) on[e] = (__bf16)(float)(sees[t] >> e & 1);
-                            bad[t] = mfma(is, on, bad[t]);
+                        if (power_is_nan(power[e])) {
+                            spoilt |= 1u << e;
+                            power[e] = 1.0f;
                         }
-                    }
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) bad[t] = mfma(bits(spoilt), bits(sees[t]), bad[t]);
                 }
-                b8 p[NT][NP];
+                float w[NT][8];
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     // NaN where a score is: the row's maximum then stays as it is,
@@ -442,39 +462,37 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
                         top = fmaxf(top, __shfl_xor(top, 16));
                         top = fmaxf(top, __shfl_xor(top, 32));
                         const bool none = raise[t] == -INFINITY;
-                        const float most = none ? top : fmaxf(sub[t], top), by = none ? 0.0f : exp2f(sub[t] - most);
+                        const float most = none ? top : fmaxf(sub[t] + kAtLift, top), by = none ? 0.0f : exp2f(sub[t] + kAtLift - most);
                         if (most != -INFINITY) {
-                            sub[t] = most;
+                            sub[t] = most - kAtLift;
                             raise[t] = most + kAtSlack;
 #pragma unroll
                             for (int r = 0; r < ND; ++r) o[t][r] *= by;
                             l[t] *= by;
                         }
                     }
-                    float w[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e / 4][e % 4], a.scale_log2, -sub[t]));
-                    if constexpr (PACK) p[t][0] = part_of<kSkip>(w, skip);
-                    else parts<NP>(w, p[t]);
-#pragma unroll
-                    for (int n = NP - 1; n >= 0; --n) l[t] = mfma(ones, p[t][n], l[t]);
+                    for (int e = 0; e < 8; ++e) w[t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e / 4][e % 4], a.scale_log2, -sub[t]));
                 }
-                add_values<DP, NT, NP>(values.w, power, p, o);
+                add_products<DP, NT, kHalf ? NH : NP, V8>(values.w, power, w, l, o);
                 there = next_there;
                 missing |= !there;
             }
             if (missing && lane == 0) atomicOr(a.c.err, kErrKvPage);
         }
-        if (care) break;
-        bool nan = false;
+        if constexpr (!kCareful && !kHalf) {
+            bool nan = false;
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int r = 0; r < ND; ++r)
+                for (int r = 0; r < ND; ++r)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) nan |= o[t][r][e] != o[t][r][e];
-        if (!__any(nan)) break;
-    }
+                    for (int e = 0; e < 4; ++e) nan |= o[t][r][e] != o[t][r][e];
+            fits = !__any(nan);
+        }
+        return fits;
+    };
+    if (!pass(std::false_type())) pass(std::true_type());
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -493,7 +511,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
     for (int t = 0; t < NT; ++t) {
         if (t) __syncthreads();
         if (lane < 16) {
-            sm[wave][lane] = raise[t] == -INFINITY ? -INFINITY : sub[t];
+            sm[wave][lane] = raise[t] == -INFINITY ? -INFINITY : sub[t] + kAtLift;
             sl[wave][lane] = l[t][0];
         }
 #pragma unroll
@@ -515,13 +533,6 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
                 by[w] = at_weight(sm[w][c], sl[w][c], most);
                 sum += by[w] * sl[w][c];
             }
-            // the parts of a row (a lane's column and those beside it)
-            if constexpr (PACK) {
-                float all = sum;
-#pragma unroll
-                for (int n = 1; n <= kSkip; ++n) all += __shfl(sum, (c + n * kAtPackRows<T>) % 16);
-                sum = all;
-            }
             const float scale = a.splits > 1 ? 1.0f : (sum == 0.0f ? 0.0f : 1.0f / sum);
 #pragma unroll
             for (int w = 0; w < NW; ++w) sm[w][c] = by[w] * scale;
@@ -534,14 +545,9 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
             f8 v = {};
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
-                const float by = sm[w][c];
-#pragma unroll
-                for (int n = 0; n <= (PACK ? kSkip : 0); ++n) {
-                    f8 y;
-                    __builtin_memcpy(&y, __builtin_assume_aligned(&lds[(w * 16 + c + n * kAtPackRows<T>) * kPitch + d], 16), sizeof y);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] += by * y[e];
-                }
+                f8 y;
+                __builtin_memcpy(&y, __builtin_assume_aligned(&lds[(w * 16 + c) * kPitch + d], 16), sizeof y);
+                v += sm[w][c] * y;
             }
             if (a.splits == 1) {
                 if (d < a.c.dim) write_row<T>(a, b, head, row0 + t * 16 + c, d, v);
@@ -667,16 +673,8 @@ static void launch_nt(const AttendArgs& a, hipStream_t st) {
     constexpr int kThreads = 64 * kAtWaves<DP, T, NT>;
     const dim3 grid((unsigned)(groups * a.splits));
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, a); };
-    if constexpr (NT == 1) {
-        if (rows <= kAtPackRows<T>) {
-            if (a.mask) launch(k_attend<DP, T, NT, true, true>);
-            else launch(k_attend<DP, T, NT, false, true>);
-            if (a.splits > 1) join<DP, T, NT>(a, st);
-            return;
-        }
-    }
-    if (a.mask) launch(k_attend<DP, T, NT, true, false>);
-    else launch(k_attend<DP, T, NT, false, false>);
+    if (a.mask) launch(k_attend<DP, T, NT, true>);
+    else launch(k_attend<DP, T, NT, false>);
     if (a.splits > 1) join<DP, T, NT>(a, st);
 }
 

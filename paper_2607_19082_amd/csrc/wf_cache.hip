@@ -65,7 +65,7 @@ __device__ __forceinline__ void load8(const T* p, int m, float (&x)[8]) {
 __device__ __forceinline__ unsigned kv_power(unsigned top, float& inv) {
     const bool nan = top >= 0x7f800000u;
     int e = (int)((top + 0x3fffffu) >> 23) - 129;
-    e = e < -kKvMaxPower ? -kKvMaxPower : (e > kKvMaxPower ? kKvMaxPower : e);
+    e = top == 0 ? 0 : (e < -kKvMaxPower ? -kKvMaxPower : (e > kKvMaxPower ? kKvMaxPower : e));
     inv = nan ? 0.0f : __builtin_bit_cast(float, (unsigned)(127 - e) << 23);   // exact: a power of two
     return nan ? kKvNan : e + 127;
 }

@@ -282,6 +282,27 @@ def test_what_a_row_does_not_see(dim, dtype):
     c.close()
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("dim,n,group,L", [(64, 1, 2, 300), (128, 3, 1, 600), (256, 1, 1, 90), (128, 400, 4, 70)])
+def test_values_of_any_size(dim, n, group, L, dtype):
+    """Values from 2^-100 to 2^100, in one channel or from token to token; the
+    huge ones at tokens that other rows see or none sees change nothing else."""
+    g = np.random.default_rng(11)
+    heads = 8 if n > 100 else 2
+    k, q = draw((1, L, heads, dim), dtype, 1), draw((1, n, heads * group, dim), dtype, 3, 0.0)
+    for sizes in (2.0 ** g.integers(-100, 101, (L, heads, 1)), 2.0 ** -100 * np.ones((L, heads, 1)), 2.0 ** 100 * np.ones((L, heads, 1)),
+                  2.0 ** g.integers(-100, 101, (1, heads, dim // 32)).repeat(32, -1).repeat(L, 0)):
+        v = torch.from_numpy((g.standard_normal((L, heads, dim)) * sizes).astype(np.float32))[None].to(DTYPE[dtype])
+        c, table = filled(k, v)
+        kq, vq = oracle.quantise(k.float().numpy()), oracle.quantise(v.float().numpy())
+        vis = g.integers(0, L + 1, (1, n))
+        vis[0, -1] = L - 5
+        out = c.attend(q.cuda(), table, ints(vis), max_visible=L)
+        c.sync()
+        check(out, q, kq, vq, vis, dtype)
+        c.close()
+
+
 def test_last_bits_of_fp32_queries_count():
     """A score of 1 that is the difference of two channels' 2^18: it needs the
     24 bits of the query, and the kernel's parts carry them."""
