@@ -12,7 +12,7 @@ GRID = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
 
 def power(top):
     """The least e in [-125, 125] with 6 * 2^e >= top, by search."""
-    e = -125
+    e = max(-125, min(125, int(np.floor(np.log2(top))) - 6)) if top > 0 else -125
     while e < 125 and 6.0 * 2.0 ** e < top:
         e += 1
     return e
@@ -36,12 +36,10 @@ def quantise(x):
     for d in range(0, x.shape[-1], BLOCK):
         b = rows[:, d:d + BLOCK]
         top = np.abs(b).max(-1)
-        for r in range(len(b)):
-            if not np.isfinite(top[r]):
-                dst[r, d:d + BLOCK] = np.nan
-                continue
-            p = 2.0 ** power(top[r])
-            dst[r, d:d + BLOCK] = GRID[nearest(b[r] / p)] * np.sign(b[r]) * p
+        sizes, which = np.unique(np.where(np.isfinite(top), top, 0.0), return_inverse=True)
+        p = np.array([2.0 ** power(t) for t in sizes])[which.reshape(-1)][:, None]
+        held = GRID[nearest(np.where(np.isfinite(b), b, 0.0) / p)] * np.sign(b) * p
+        dst[:, d:d + BLOCK] = np.where(np.isfinite(top)[:, None], held, np.nan)
     return out
 
 

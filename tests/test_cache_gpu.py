@@ -225,6 +225,28 @@ def test_attend_long(dim, n, group, L, page, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("dim,n,heads,group,lens", [
+    (64, 1, 3, 1, [5000, 0, 3, 0, 0, 33, 700, 1]), (128, 1, 2, 4, [0, 0, 900, 64, 2100]), (256, 2, 1, 3, [300, 301, 0]),
+    (128, 3, 1, 5, [40] * 50 + [1500] + [0] * 20), (64, 2, 2, 1, [0, 0]), (128, 1, 1, 16, [1024] * 6),
+    (96, 1, 1, 8, list(range(0, 400, 7))), (64, 1, 8, 1, [17] * 256)])
+def test_batches_of_any_lengths(dim, n, heads, group, lens, dtype):
+    """A token or two of many sequences: one long among short ones, none, equal
+    ones, as many as a launch takes together."""
+    B, L = len(lens), max(max(lens), 1)
+    g = np.random.default_rng(3)
+    k, v = draw((B, L, heads, dim), dtype, 1), draw((B, L, heads, dim), dtype, 2)
+    q = draw((B, n, heads * group, dim), dtype, 3, 0.0)
+    c, table = filled(k, v)
+    vis = np.array([[m if i == 0 else g.integers(0, m + 1) for i in range(n)] for m in lens])
+    out = torch.full_like(q.cuda(), 9.0)
+    c.attend(q.cuda(), table, ints(vis), max_visible=L, out=out)
+    c.sync()
+    check(out, q, oracle.quantise(k.float().numpy()), oracle.quantise(v.float().numpy()), vis, dtype)
+    assert torch.equal(out, c.attend(q.cuda(), table, ints(vis), max_visible=L))
+    c.close()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("dim,n,group,L", [(64, 3, 1, 95), (128, 2, 4, 1500), (96, 34, 3, 333), (256, 1, 2, 64)])
 def test_mask(dim, n, group, L, dtype):
     """Masks: random, a row that allows nothing, a row that allows one token;
@@ -280,6 +302,45 @@ def test_what_a_row_does_not_see(dim, dtype):
     assert got[2].sum() == 64 and got[4].all()
     check(out, q, kq, vq, vis, dtype, m)
     c.close()
+
+
+@pytest.mark.parametrize("dim,n,group,heads,B", [(64, 130, 1, 2, 1), (128, 70, 3, 1, 2), (96, 64, 2, 1, 1), (64, 33, 8, 1, 1),
+                                                 (128, 300, 1, 3, 1)])
+def test_many_rows(dim, n, group, heads, B):
+    """Many rows of unequal prefixes, some that see nothing or all; a key and
+    values that are not finite at tokens that some of them see; a page outside
+    the pool."""
+    g = np.random.default_rng(7)
+    L = 700
+    k, v = draw((B, L, heads, dim), "bf16", 1), draw((B, L, heads, dim), "bf16", 2)
+    q = draw((B, n, heads * group, dim), "bf16", 3, 0.0)
+    for bad in (False, True):
+        if bad:
+            k[:, 600, :, 3] = float("nan")
+            v[:, 500, :, 5] = float("inf")
+            v[:, 501, :, dim - 1] = float("nan")
+            k[0, 690:], v[0, 690:] = float("nan"), float("nan")
+        c, table = filled(k, v)
+        kq, vq = oracle.quantise(k.float().numpy()), oracle.quantise(v.float().numpy())
+        vis = g.integers(0, L + 1, (B, n))
+        vis[:, :3] = [[L, 0, 500]]
+        vis[0, n // 2:] = np.minimum(vis[0, n // 2:], 500)
+        if bad:
+            vis[0] = np.minimum(vis[0], 690)
+        out = c.attend(q.cuda(), table, ints(vis), max_visible=L)
+        c.sync()
+        check(out, q, kq, vq, vis, "bf16")
+        assert torch.equal(out.nan_to_num(7.0), c.attend(q.cuda(), table, ints(vis), max_visible=L).nan_to_num(7.0))
+        if not bad:
+            broken = table.clone()
+            broken[:, 4] = 1 << 30
+            out = c.attend(q.cuda(), broken, ints(vis), max_visible=L)
+            with pytest.raises(wf.WfError):
+                c.sync()
+            mask = np.ones((B, n, L), bool)
+            mask[:, :, 256:320] = False
+            check(out, q, kq, vq, vis, "bf16", mask)
+        c.close()
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
