@@ -6,6 +6,7 @@ current HIP stream.  It raises if the library is missing; there is no fallback.
 """
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -66,8 +67,10 @@ class CacheDesc(ctypes.Structure):
                 ("page", ctypes.c_int32)]
 
 
-# wf_rows: a pointer and three strides, as four words
+# wf_rows: a pointer and three strides, as four words (an array of them, or
+# packed into bytes, which is quicker to make)
 Rows = ctypes.c_int64 * 4
+_pack_rows = struct.Struct("4q").pack
 
 
 class Out(ctypes.Structure):
@@ -492,11 +495,11 @@ class Cache:
 
     @staticmethod
     def _rows(t, shape, dtype, name):
-        st = t.stride()
-        if not t.is_cuda or t.dtype != dtype or t.shape != shape or (st[3] != 1 and t.numel()):
+        if not t.is_cuda or t.dtype != dtype or t.shape != shape or (t.stride(3) != 1 and t.numel()):
             raise ValueError(f"{name}: expected a {dtype} CUDA tensor {tuple(shape)} with contiguous channels, got "
-                             f"{t.dtype} {tuple(t.shape)}, strides {st}, on {t.device}")
-        return Rows(t.data_ptr(), st[0], st[1], st[2])
+                             f"{t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
+        sequence, token, head, _ = t.stride()
+        return _pack_rows(t.data_ptr(), sequence, token, head)
 
     def _ints(self, t, shape, name):
         if not t.is_cuda or t.dtype != self._torch.int32 or t.shape != shape or not t.is_contiguous():
@@ -516,8 +519,8 @@ class Cache:
         pages = table.shape[1]
         return self._ints(table, (B, pages), "table"), pages
 
-    def _empty(self, shape, dtype, device, stream):
-        t = self._torch.empty(shape, dtype=dtype, device=device)
+    def _empty(self, shape, dtype, device, stream, like=None):
+        t = self._torch.empty(shape, dtype=dtype, device=device) if like is None else self._torch.empty_like(like)
         if stream is not None:          # allocated on the current stream, used on another
             t.record_stream(stream)
         return t
@@ -549,9 +552,11 @@ class Cache:
         shape = (B, n, self.heads, self.dim)
         if out is None:
             dtype = self._torch.float32 if dtype is None else dtype
-            out = (self._empty(shape, dtype, table.device, stream), self._empty(shape, dtype, table.device, stream))
-        k, v = out
-        dtype = k.dtype
+            k = self._empty(shape, dtype, table.device, stream)
+            v = self._empty(shape, dtype, table.device, stream, like=k)
+        else:
+            k, v = out
+            dtype = k.dtype
         rc = self._lib.wf_cache_read(
             self._h, self._type(dtype), self._rows(k, shape, dtype, "k"), self._rows(v, shape, dtype, "v"), B, n, p_table,
             pages, self._ints(first, (B,), "first"), None if counts is None else self._ints(counts, (B,), "counts"),
@@ -576,7 +581,7 @@ class Cache:
         if max_visible is None:
             max_visible = pages * self.page if mask is None else mask.shape[-1]
         if out is None:
-            out = self._empty(shape, dtype, q.device, stream)
+            out = self._empty(shape, dtype, q.device, stream, like=q if q.is_contiguous() else None)
         p_mask = strides = None
         if mask is not None:
             if not mask.is_cuda or mask.dtype != self._torch.bool or mask.shape != (B, n, max_visible) or \
