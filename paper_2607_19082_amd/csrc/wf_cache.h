@@ -108,6 +108,7 @@ struct AttendArgs {
     long long mb, mr;                // mask strides: sequence, row
     int table_pages, B, n, group;    // group: query heads of a key head
     int max_visible, splits;
+    int ahead;                       // > 0: sequences by length, this many from the longest down
     float scale_log2;                // scale * log2(e)
     float *part_o, *part_ml;         // partial results: channels, and (maximum, sum)
 };
