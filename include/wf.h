@@ -487,8 +487,8 @@ void wf_xform_destroy(wf_xform_t plan);
  * Format: a block of 32 consecutive channels of one token's head (the last
  * block of a head may be shorter) holds 4-bit values {0, 1/2, 1, 3/2, 2, 3, 4,
  * 6} with a sign, times 2^e: e is the least integer in [-125, 125] with
- * 6 * 2^e >= the block's largest magnitude, and x / 2^e is rounded to the
- * nearest value, a tie to the even code (magnitudes beyond 6 * 2^125 are held
+ * 6 * 2^e >= the block's largest magnitude, so that nothing is cut off, and
+ * x / 2^e is rounded to the nearest value, a tie to the even code (magnitudes beyond 6 * 2^125 are held
  * as that).  A block with a value that is not finite reads back as NaN.  4.25
  * bits a value; the bytes' order in a page is the library's own.
  *
@@ -559,8 +559,9 @@ int wf_cache_read(wf_cache_t cache, int32_t precision, const wf_rows *k, const w
  *                cut there, and the next wf_cache_sync returns WF_E_CAPACITY
  *   scale        positive; 1 / sqrt(dim) as a rule
  * Tokens in a page outside the pool are left out, and the next wf_cache_sync
- * returns WF_E_INVALID.  Sums are held in fp32, and their order depends on the
- * call's sizes alone.  Asynchronous on `stream`; one call in flight per cache
+ * returns WF_E_INVALID.  Sums are held in fp32, before they are divided (they
+ * overflow where |v| is beyond about 2^112 / the row's tokens), and their order
+ * depends on the call's sizes alone.  Asynchronous on `stream`; one call in flight per cache
  * (the workspace is shared by its calls).
  */
 int wf_cache_attend(wf_cache_t cache, int32_t precision, const wf_rows *q, const wf_rows *out, int32_t B, int32_t n,

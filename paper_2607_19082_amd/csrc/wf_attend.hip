@@ -16,12 +16,22 @@
 // Operands: keys and values are exact in bf16.  bf16 queries are too; fp32
 // queries are three bf16 parts (24 bits).  Probabilities are two bf16 parts
 // (16 bits) for bf16 calls, so that the output's own rounding is the only one
-// that shows, and three (24 bits) for fp32 calls.  Scores, maxima, sums and
-// outputs are held in fp32; a row's sum is that of its rounded probabilities.
+// that shows.  For fp32 calls they are two parts in half precision (22 bits),
+// with values in half precision too, where the values' powers allow that, and
+// three bf16 parts otherwise.  Scores, maxima, sums and outputs are held in
+// fp32; a row's sum is that of its rounded probabilities.
 //
-// The four waves of a workgroup share the tokens and join at the end; with
-// few rows the tokens are also split over workgroups, and a second kernel
-// joins their results.
+// The waves of a workgroup share the tokens and join at the end; with few rows
+// the tokens are also split over workgroups, and a second kernel joins their
+// results.
+//
+// What bounds it (8 heads of 128, bf16, MI355X): a token each of 32 sequences
+// of 8192 tokens, 4 query heads a key head, takes 57 us for 286 MB, 5.0 TB/s
+// where a kernel that only reads reaches 5.7.  A tile costs a wave ~170 vector
+// instructions, 96 of them conversions and the exchange of values between
+// tokens, and 26 products; the two hardly overlap, so with many rows (1024
+// queries, 32 heads, 16384 tokens: 380 us, 0.70 PFLOP/s) their sum is the time,
+// and with few tokens a wave (1001 in all: 9 us) the chain of one tile is.
 #include <cmath>
 #include <type_traits>
 
@@ -41,10 +51,15 @@ typedef unsigned u2 __attribute__((ext_vector_type(2)));
 // read-only for the whole launch, at addresses that a wave shares: scalar loads
 typedef const int __attribute__((address_space(4))) * SharedInts;
 
-constexpr int kAtTarget = 256;      // workgroups that a call is split into
+// Workgroups that a call is split into: one for each compute unit.  us for 192
+// / 256 / 320 / 512: one token over 131072 36 / 35 / 42 / 36; 45 fp32 rows over
+// 32300 19 / 17 / 21 / 18; 56 fp32 rows of 256 channels over 20011 30 / 26 / 38
+// / 34 (the last ones wait for a place, and the join has more to read).
+constexpr int kAtTarget = 256;
 constexpr int kAtMaxSplits = 256;
 constexpr int kAtJoin = 256;        // threads of the kernel that joins the splits
-// waves of a workgroup
+// Waves of a workgroup.  (16 instead of 8: 10.2 against 9.1 us for a token over
+// 1001, since the larger workgroup starts later.)
 template <int DP, class T, int NT>
 constexpr int kAtWaves = NT == 1 && DP * sizeof(T) < 1024 ? 8 : 4;
 // a row's maximum is raised only when a score passes it by this much (in
@@ -270,9 +285,9 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, int b, int head, 
     __builtin_memcpy((T*)a.o.p + b * a.o.sb + i * a.o.sr + h * a.o.sh + d, out, sizeof out);
 }
 
-// Waves of a SIMD that the registers are shared out for.
+// Waves of a SIMD that the registers are shared out for (none spills).
 template <int DP, class T, int NT>
-constexpr int kAtWgs = NT == 1 && DP * (int)sizeof(T) <= 256 ? 4 : NT * DP * (int)sizeof(T) <= 128 * 2 ? 3 : (NT * DP * (int)sizeof(T) <= 256 * 2 ? 2 : 1);
+constexpr int kAtWavesOfSimd = NT == 1 && DP * sizeof(T) <= 256 ? 4 : (NT * DP * sizeof(T) <= 256 ? 3 : (NT * DP * sizeof(T) <= 512 ? 2 : 1));
 
 constexpr int kAtBatch = 256;       // sequences that are taken by length, at most
 
@@ -301,7 +316,7 @@ __device__ __forceinline__ int by_length(const AttendArgs& a, int place, int ahe
 // One workgroup: 16 NT rows of a sequence's key head, and a share of its
 // tokens.
 template <int DP, class T, int NT, bool MASK>
-__global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) void k_attend(AttendArgs a) {
+__global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, NT>)) void k_attend(AttendArgs a) {
     constexpr int NW = kAtWaves<DP, T, NT>, NQ = AtParts<T>::kQ, NP = AtParts<T>::kP, NH = AtParts<T>::kH, NK = DP / 32, ND = DP / 16;
     using L = KvLayout<DP>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
@@ -530,7 +545,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
 
     // join the waves, one tile of 16 rows after the other
     constexpr int kPitch = DP + 4, W = DP / 8, kThreads = 64 * NW;
-    __shared__ float lds[NW * 16 * kPitch];
+    __shared__ __attribute__((aligned(16))) float lds[NW * 16 * kPitch];
     __shared__ float sm[NW][16], sl[NW][16], top[16];
     const int row0 = rt * 16 * NT, here = min(16 * NT, rows - row0);
     const size_t part = (((size_t)(b * a.c.heads + head) * nrt + group % nrt) * a.splits + split) * 16 * NT;
@@ -596,7 +611,8 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWgs<DP, T, NT>)) vo
 template <int DP, class T>
 __global__ __launch_bounds__(kAtJoin) void k_attend_join(AttendArgs a, int tile_rows) {
     constexpr int W = DP / 8, G = kAtJoin / W, K = kAtMaxSplits / 64, Y = 4;
-    __shared__ float weight[kAtMaxSplits], so[kAtJoin / 64][DP];
+    __shared__ float weight[kAtMaxSplits];
+    __shared__ __attribute__((aligned(16))) float so[kAtJoin / 64][DP];
     const unsigned rows = a.n * a.group, row = blockIdx.x % rows, bh = blockIdx.x / rows;
     const int g = threadIdx.x / W, d = threadIdx.x % W * 8, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const unsigned nrt = (rows + tile_rows - 1) / tile_rows;
@@ -659,27 +675,29 @@ __global__ __launch_bounds__(kAtJoin) void k_attend_join(AttendArgs a, int tile_
 
 // ---- host -----------------------------------------------------------------------
 
-// Column tiles of a workgroup: two where they fit the registers without spills
-// and there are enough rows to fill the chip all the same.  us with one / two, 8
-// heads of 128, 16384 tokens, bf16: 64 tiles 28 / 30, 256 78 / 77, 512 149 /
-// 130, 2048 520 / 393; 5 heads of 64, 8192 tokens, fp32: 20 tiles 15 / 19, 160
-// 47 / 40, 320 71 / 66.  (Two of 128 channels in fp32 gain nothing: 2048 tiles
-// 382 / 385; nor do four of 64 in bf16: 320 tiles 49 / 50, four 52.)
+// Column tiles of a workgroup: two, which share a tile's conversions, where they
+// fit the registers and there are enough rows to fill the chip all the same.
+// us with one / two, 8 heads, 8192 tokens: of 128 in bf16, 256 tiles of rows 40
+// / 46, 512 72 / 65, 1024 135 / 110, 2048 248 / 203; of 64 in bf16, 512 48 /
+// 50, 768 69 / 74, 1024 85 / 74; of 64 in fp32, 512 58 / 57, 768 80 / 86, 1024
+// 102 / 91.  Hence tiles times channels.
 template <int DP, class T>
 constexpr bool kAtTwoTiles = DP * sizeof(T) <= 256;
-constexpr long long kAtManyTiles = 512;
+constexpr long long kAtManyRows = 1 << 16;
 
 static int row_tiles(const AttendArgs& a, int precision) {
     const int rows = a.n * a.group;
     const long long tiles = (long long)a.B * a.c.heads * ((rows + 15) / 16);
-    return rows > 16 && tiles >= kAtManyTiles && a.c.dp * (precision == WF_BF16 ? 2 : 4) <= 256 ? 2 : 1;
+    return rows > 16 && tiles * a.c.dp >= kAtManyRows && a.c.dp * (precision == WF_BF16 ? 2 : 4) <= 256 ? 2 : 1;
 }
 
 void attend_plan(AttendArgs& a, int precision) {
     const int bytes = a.c.dp * (precision == WF_BF16 ? 2 : 4), nt = row_tiles(a, precision), rows = a.n * a.group;
     const int waves = nt == 1 && bytes < 1024 ? 8 : 4;
     const long long groups = (long long)a.B * a.c.heads * ((rows + 16 * nt - 1) / (16 * nt));
-    // workgroups that keep the chip busy, with at least four tiles for each wave
+    // at least four tiles for each wave, below which the join costs more than
+    // the split gains (68 masked rows over 8101 tokens: 16.4 us with one, 17.0
+    // with four, 18.4 with six; a token over 1001 10.2 with one, 9.1)
     long long s = kAtTarget / groups;
     const long long by_len = a.max_visible / (4 * waves * kKvTile);
     s = s < by_len ? s : by_len;

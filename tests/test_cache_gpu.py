@@ -343,6 +343,32 @@ def test_many_rows(dim, n, group, heads, B):
         c.close()
 
 
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("dim,n,group,heads,B,dtype", [(128, 256, 4, 8, 1, "bf16"), (128, 130, 4, 8, 2, "bf16"), (64, 515, 4, 8, 1, "bf16"),
+                                                       (64, 512, 4, 8, 1, "fp32"), (96, 70, 1, 16, 8, "bf16")])
+def test_rows_that_fill_the_chip(dim, n, group, heads, B, dtype, masked):
+    """Enough rows for a workgroup to take two tiles of them: unequal prefixes,
+    values that are not finite or far apart in size, a mask."""
+    g = np.random.default_rng(13)
+    L = 75
+    k, v = draw((B, L, heads, dim), dtype, 1), draw((B, L, heads, dim), dtype, 2)
+    q = draw((B, n, heads * group, dim), dtype, 3, 0.0)
+    v[:, 10, 1] *= 2.0 ** 60
+    v[:, 50, 2, 7] = float("nan")
+    k[:, 51, 3, 1] = float("inf")
+    k[:, 70:], v[:, 70:] = float("nan"), float("nan")
+    c, table = filled(k, v)
+    kq, vq = oracle.quantise(k.float().numpy()), oracle.quantise(v.float().numpy())
+    vis = g.integers(0, 71, (B, n))
+    vis[:, :2] = [[70, 0]]
+    vis[:, n // 2:] = np.minimum(vis[:, n // 2:], 50)
+    m = g.random((B, n, L)) < 0.4 if masked else None
+    out = c.attend(q.cuda(), table, ints(vis), max_visible=L, mask=torch.from_numpy(m).cuda() if masked else None)
+    c.sync()
+    check(out, q, kq, vq, vis, dtype, m)
+    c.close()
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("dim,n,group,L", [(64, 1, 2, 300), (128, 3, 1, 600), (256, 1, 1, 90), (128, 400, 4, 70)])
 def test_values_of_any_size(dim, n, group, L, dtype):
