@@ -249,6 +249,7 @@ void launch_kv_read(const KvCache& c, int precision, const KvRows& k, const KvRo
 
 struct Cache {
     KvCache c{};
+    void* memory = nullptr;          // one allocation: the error word, the pool, the workspace
     float* work = nullptr;           // partial results of split attention calls
 };
 
@@ -256,9 +257,7 @@ static int kv_fail(hipError_t e, const char* what) { return fail(WF_E_HIP, std::
 
 static void free_cache(Cache* c) {
     if (!c) return;
-    if (c->c.pool) (void)hipFree(c->c.pool);
-    if (c->c.err) (void)hipFree(c->c.err);
-    if (c->work) (void)hipFree(c->work);
+    if (c->memory) (void)hipFree(c->memory);
     delete c;
 }
 
@@ -309,17 +308,20 @@ int wf_cache_plan(const wf_cache_desc* d, wf_cache_t* out) {
     k.heads = d->heads; k.dim = d->dim; k.pages = d->pages;
     k.dp = d->dim <= 64 ? 64 : (d->dim <= 128 ? 128 : 256);
     while ((1 << k.page_shift) < d->page) ++k.page_shift;
-    const size_t bytes = k.page_bytes() * k.pages;
-    hipError_t e = hipMalloc((void**)&k.pool, bytes);
-    if (e == hipSuccess) e = hipMalloc((void**)&k.err, sizeof(int));
-    if (e == hipSuccess) e = hipMalloc((void**)&c->work, (size_t)kAttendWorkRows * (k.dp + 2) * sizeof(float));
+    // (a record is a multiple of 64 bytes)
+    const size_t head = 256, pool = (k.page_bytes() * k.pages + 255) / 256 * 256;
+    const size_t work = (size_t)kAttendWorkRows * (k.dp + 2) * sizeof(float);
+    hipError_t e = hipMalloc(&c->memory, head + pool + work);
     if (e != hipSuccess) {
+        c->memory = nullptr;
         free_cache(c);
         return fail(WF_E_NOMEM, std::string("cache: ") + hipGetErrorString(e));
     }
-    // a page that is never written reads as zeros
-    e = hipMemset(k.pool, 0, bytes);
-    if (e == hipSuccess) e = hipMemset(k.err, 0, sizeof(int));
+    k.err = static_cast<int*>(c->memory);
+    k.pool = static_cast<uint8_t*>(c->memory) + head;
+    c->work = reinterpret_cast<float*>(k.pool + pool);
+    // no error, and a page that is never written reads as zeros
+    e = hipMemset(c->memory, 0, head + pool);
     if (e == hipSuccess) e = hipDeviceSynchronize();
     if (e != hipSuccess) {
         free_cache(c);
