@@ -607,7 +607,9 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
 
 // Joins the splits of one row: eight channels a lane, the splits dealt to
 // groups of lanes.  The first wave turns the splits' maxima and sums into
-// weights while the partial results are on their way.
+// weights while the partial results are on their way.  Bound by its chain of
+// launch, load and two exchanges: 3.9 us for 225 rows in 17 splits, 4.7 for 32
+// rows in 32.
 template <int DP, class T>
 __global__ __launch_bounds__(kAtJoin) void k_attend_join(AttendArgs a, int tile_rows) {
     constexpr int W = DP / 8, G = kAtJoin / W, K = kAtMaxSplits / 64, Y = 4;

@@ -82,7 +82,10 @@ __device__ __forceinline__ unsigned kv_code(const float (&x)[8], float inv) {
 }
 
 // Lanes take eight channels of a token each, the token's first, then the next
-// token: four lanes share a block.  Bound by memory.
+// token: four lanes share a block, and find its largest magnitude in two
+// exchanges.  Bound by memory: two prompts of 8191 tokens, 8 heads of 128 in
+// bf16, take 17 us for 67 MB read and 18 written, 5.0 TB/s; a token 3.6 us, the
+// chain of its loads.
 template <int DP, class T>
 __global__ __launch_bounds__(kKvThreads) void k_kv_write(KvCache c, KvRows k, KvRows v, KvTokens a) {
     using L = KvLayout<DP>;
@@ -313,6 +316,7 @@ int wf_cache_plan(const wf_cache_desc* d, wf_cache_t* out) {
     const size_t work = (size_t)kAttendWorkRows * (k.dp + 2) * sizeof(float);
     hipError_t e = hipMalloc(&c->memory, head + pool + work);
     if (e != hipSuccess) {
+        (void)hipGetLastError();     // reported here, not by the next launch
         c->memory = nullptr;
         free_cache(c);
         return fail(WF_E_NOMEM, std::string("cache: ") + hipGetErrorString(e));

@@ -463,7 +463,7 @@ class Cache:
     pages, page  pages of the pool, tokens of a page (a power of two, 32 to 1024)
 
     Token t of sequence b lies in page table[b, t // page].  Tensors are torch
-    tensors on the current HIP device, fp32 or bf16 where they hold channels
+    tensors on the HIP device that was current at the plan, fp32 or bf16 where they hold channels
     (contiguous; sequence, token and head may have any strides) and contiguous
     int32 elsewhere.  Calls are asynchronous on the given (default: current)
     torch stream; one attend call in flight per cache.  sync() waits and raises
@@ -474,6 +474,7 @@ class Cache:
         h = ctypes.c_void_p()
         _check(lib().wf_cache_plan(ctypes.byref(CacheDesc(heads, dim, pages, page)), ctypes.byref(h)))
         self._h = h
+        self._device = torch.cuda.current_device()
         self.heads, self.dim, self.pages, self.page = heads, dim, pages, page
         # a serving step makes several short calls: what they look up is kept
         self._lib, self._torch = lib(), torch
@@ -493,18 +494,17 @@ class Cache:
         except Exception:
             pass
 
-    @staticmethod
-    def _rows(t, shape, dtype, name):
-        if not t.is_cuda or t.dtype != dtype or t.shape != shape or (t.stride(3) != 1 and t.numel()):
-            raise ValueError(f"{name}: expected a {dtype} CUDA tensor {tuple(shape)} with contiguous channels, got "
-                             f"{t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
+    def _rows(self, t, shape, dtype, name):
+        if t.get_device() != self._device or t.dtype != dtype or t.shape != shape or (t.stride(3) != 1 and t.numel()):
+            raise ValueError(f"{name}: expected a {dtype} tensor {tuple(shape)} on device {self._device} with contiguous "
+                             f"channels, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
         sequence, token, head, _ = t.stride()
         return _pack_rows(t.data_ptr(), sequence, token, head)
 
     def _ints(self, t, shape, name):
-        if not t.is_cuda or t.dtype != self._torch.int32 or t.shape != shape or not t.is_contiguous():
-            raise ValueError(f"{name}: expected a contiguous int32 CUDA tensor {tuple(shape)}, got {t.dtype} "
-                             f"{tuple(t.shape)} on {t.device}")
+        if t.get_device() != self._device or t.dtype != self._torch.int32 or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name}: expected a contiguous int32 tensor {tuple(shape)} on device {self._device}, got "
+                             f"{t.dtype} {tuple(t.shape)} on {t.device}")
         return t.data_ptr()
 
     def _type(self, dtype):
@@ -584,10 +584,11 @@ class Cache:
             out = self._empty(shape, dtype, q.device, stream, like=q if q.is_contiguous() else None)
         p_mask = strides = None
         if mask is not None:
-            if not mask.is_cuda or mask.dtype != self._torch.bool or mask.shape != (B, n, max_visible) or \
+            if mask.get_device() != self._device or mask.dtype != self._torch.bool or mask.shape != (B, n, max_visible) or \
                     (max_visible > 1 and mask.stride(2) != 1):
-                raise ValueError(f"mask: expected a bool CUDA tensor {(B, n, max_visible)} with contiguous tokens, got "
-                                 f"{mask.dtype} {tuple(mask.shape)}, strides {mask.stride()}")
+                raise ValueError(f"mask: expected a bool tensor {(B, n, max_visible)} on device {self._device} with "
+                                 f"contiguous tokens, got {mask.dtype} {tuple(mask.shape)}, strides {mask.stride()}, on "
+                                 f"{mask.device}")
             p_mask, strides = mask.data_ptr(), (ctypes.c_int64 * 2)(mask.stride(0), mask.stride(1))
         rc = self._lib.wf_cache_attend(
             self._h, self._type(dtype), self._rows(q, shape, dtype, "q"), self._rows(out, shape, dtype, "out"), B, n, hq,

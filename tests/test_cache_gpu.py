@@ -540,3 +540,15 @@ def test_refusals():
     assert (c.attend(q + 1, table, 0 * vis, max_visible=0) == 0).all()
     c.sync()
     c.close()
+
+
+def test_a_pool_that_does_not_fit():
+    with pytest.raises(wf.WfError) as e:
+        wf.Cache(8, 128, 1 << 22, page=1024)        # 4.7 TB
+    assert e.value.code == wf.WF_E_NOMEM
+    # and nothing of it is left for the calls that follow
+    k = draw((1, 40, 2, 64), "fp32", 1)
+    c, table = filled(k, k, page=32)
+    assert torch.equal(c.read(table, ints([0]), 40)[0][0].cpu(), torch.from_numpy(oracle.quantise(k[0].numpy())).float())
+    c.sync()
+    c.close()
