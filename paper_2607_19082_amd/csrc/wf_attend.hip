@@ -272,13 +272,14 @@ __device__ __forceinline__ void add_products(const unsigned (&v)[DP / 16], const
 
 // Weight of a partial result with maximum m and sum l; 0 where it saw no token.
 __device__ __forceinline__ float at_weight(float m, float l, float most) {
-    return m == -INFINITY && l == 0.0f ? 0.0f : (m == most ? 1.0f : exp2f(m - most));
+    const float w = __builtin_amdgcn_exp2f(m - most);
+    return m == -INFINITY && l == 0.0f ? 0.0f : (m == most ? 1.0f : w);
 }
 
 // Eight channels of a row, into the output.
 template <class T>
 __device__ __forceinline__ void write_row(const AttendArgs& a, int b, int head, int row, int d, const f8& v) {
-    const int i = row / a.group, h = head * a.group + row % a.group;
+    const int i = a.group_(row), h = (head - i) * a.group + row;
     T out[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) out[e] = (T)v[e];
@@ -321,10 +322,11 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     using L = KvLayout<DP>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int rows = a.n * a.group, nrt = (rows + 16 * NT - 1) / (16 * NT);
-    const int split = blockIdx.x % a.splits, group = blockIdx.x / a.splits;
-    const int rt = nrt - 1 - group % nrt;              // under a causal order the last rows see most: first
-    const int head = group / nrt % a.c.heads;
-    int b = group / nrt / a.c.heads;
+    const int group = a.splits_(blockIdx.x), split = blockIdx.x - group * a.splits;
+    const int bh = a.tiles_(group), place = group - bh * nrt;
+    const int rt = nrt - 1 - place;                    // under a causal order the last rows see most: first
+    int b = a.heads_(bh);
+    const int head = bh - b * a.c.heads;
     if constexpr (NT == 1)
         if (a.ahead) b = by_length(a, b, a.ahead);
 
@@ -336,7 +338,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     for (int t = 0; t < NT; ++t) {
         const int row = rt * 16 * NT + t * 16 + col;
         const bool on = row < rows;
-        const int i = on ? row / a.group : 0, h = head * a.group + (on ? row % a.group : 0);
+        const int i = on ? a.group_(row) : 0, h = (head - i) * a.group + (on ? row : 0);
         int s = on ? a.visible[(size_t)b * a.n + i] : 0;
         if (s > a.max_visible) {
             atomicOr(a.c.err, kErrKvRange);
@@ -363,17 +365,12 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
             parts<NQ>(x, q[t][kk]);
         }
     }
-#pragma unroll
-    for (int x = 1; x < 16; x <<= 1) {
-        most = max(most, __shfl_xor(most, x));
-        least = min(least, __shfl_xor(least, x));
-    }
-    most = __builtin_amdgcn_readfirstlane(most);
-    least = __builtin_amdgcn_readfirstlane(least);
+    most = __builtin_amdgcn_readfirstlane(lanes16(most, [](int x, int y) { return max(x, y); }));
+    least = __builtin_amdgcn_readfirstlane(lanes16(least, [](int x, int y) { return min(x, y); }));
 
     // the tiles of this split, dealt to the waves in turn
     const int tiles = (most + kKvTile - 1) / kKvTile;
-    const int share = (tiles + a.splits - 1) / a.splits;
+    const int share = a.splits_(tiles + a.splits - 1);
     const int t0 = split * share, t1 = min(tiles, t0 + share);
     const SharedInts table = (SharedInts)(a.table + (size_t)b * a.table_pages);
     const int in_page = a.c.page_shift - 5;
@@ -501,8 +498,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                     for (int e = 1; e < 8; ++e) top = __builtin_elementwise_maximum(top, s[t][e / 4][e % 4]);
                     top *= a.scale_log2;
                     if (__any(top > raise[t])) {
-                        top = fmaxf(top, __shfl_xor(top, 16));
-                        top = fmaxf(top, __shfl_xor(top, 32));
+                        top = lane_rows(top, [](float x, float y) { return fmaxf(x, y); });
                         const bool none = raise[t] == -INFINITY;
                         const float most = none ? top : fmaxf(sub[t] + kAtLift, top), by = none ? 0.0f : exp2f(sub[t] + kAtLift - most);
                         if (most != -INFINITY) {
@@ -548,7 +544,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     __shared__ __attribute__((aligned(16))) float lds[NW * 16 * kPitch];
     __shared__ float sm[NW][16], sl[NW][16], top[16];
     const int row0 = rt * 16 * NT, here = min(16 * NT, rows - row0);
-    const size_t part = (((size_t)(b * a.c.heads + head) * nrt + group % nrt) * a.splits + split) * 16 * NT;
+    const size_t part = (((size_t)(b * a.c.heads + head) * nrt + place) * a.splits + split) * 16 * NT;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         if (t) __syncthreads();
@@ -610,39 +606,38 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
 // weights while the partial results are on their way.  Bound by its chain of
 // launch, load and two exchanges: 3.9 us for 225 rows in 17 splits, 4.7 for 32
 // rows in 32.
-template <int DP, class T>
-__global__ __launch_bounds__(kAtJoin) void k_attend_join(AttendArgs a, int tile_rows) {
+template <int DP, class T, int NT>
+__global__ __launch_bounds__(kAtJoin) void k_attend_join(AttendArgs a) {
     constexpr int W = DP / 8, G = kAtJoin / W, K = kAtMaxSplits / 64, Y = 4;
     __shared__ float weight[kAtMaxSplits];
     __shared__ __attribute__((aligned(16))) float so[kAtJoin / 64][DP];
-    const unsigned rows = a.n * a.group, row = blockIdx.x % rows, bh = blockIdx.x / rows;
+    constexpr int tile_rows = 16 * NT;
+    const unsigned rows = a.n * a.group, row = blockIdx.x, bh = blockIdx.y;
     const int g = threadIdx.x / W, d = threadIdx.x % W * 8, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const unsigned nrt = (rows + tile_rows - 1) / tile_rows;
     const size_t first = ((size_t)bh * nrt + (nrt - 1 - row / tile_rows)) * a.splits * tile_rows + row % tile_rows;
     const float* po = a.part_o + first * DP + d;
+    f2 z[K];
+    if (wave == 0)
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            __builtin_memcpy(&z[k], __builtin_assume_aligned(a.part_ml + (first + (size_t)min(k * 64 + lane, a.splits - 1) * tile_rows) * 2, 8), 8);
     f8 y[Y];
 #pragma unroll
     for (int j = 0; j < Y; ++j)
         __builtin_memcpy(&y[j], __builtin_assume_aligned(po + (size_t)min(g + j * G, a.splits - 1) * tile_rows * DP, 16), 32);
+    __builtin_amdgcn_sched_barrier(0);
     if (wave == 0) {
-        f2 z[K];
         float most = -INFINITY, sum = 0.0f;
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            z[k] = f2{-INFINITY, 0.0f};
-            if (k * 64 + lane < a.splits)
-                __builtin_memcpy(&z[k], __builtin_assume_aligned(a.part_ml + (first + (size_t)(k * 64 + lane) * tile_rows) * 2, 8), 8);
-            most = fmaxf(most, z[k][0]);
-        }
-#pragma unroll
-        for (int x = 1; x < 64; x <<= 1) most = fmaxf(most, __shfl_xor(most, x));
+        for (int k = 0; k < K; ++k) most = fmaxf(most, z[k][0]);
+        most = lanes64(most, [](float x, float y) { return fmaxf(x, y); });
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            z[k][0] = at_weight(z[k][0], z[k][1], most);
+            z[k][0] = k * 64 + lane < a.splits ? at_weight(z[k][0], z[k][1], most) : 0.0f;
             sum += z[k][0] * z[k][1];
         }
-#pragma unroll
-        for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
+        sum = lanes64(sum, [](float x, float y) { return x + y; });
         const float scale = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
         for (int k = 0; k < K; ++k) weight[k * 64 + lane] = z[k][0] * scale;
@@ -650,9 +645,12 @@ __global__ __launch_bounds__(kAtJoin) void k_attend_join(AttendArgs a, int tile_
     __syncthreads();
     f8 v = {};
     for (int s = g; s < a.splits; s += Y * G) {
+        float by[Y];
+#pragma unroll
+        for (int j = 0; j < Y; ++j) by[j] = weight[min(s + j * G, kAtMaxSplits - 1)];
 #pragma unroll
         for (int j = 0; j < Y; ++j)
-            if (s + j * G < a.splits) v += weight[s + j * G] * y[j];
+            if (s + j * G < a.splits) v += by[j] * y[j];
         if (s + Y * G < a.splits)
 #pragma unroll
             for (int j = 0; j < Y; ++j)
@@ -672,7 +670,8 @@ __global__ __launch_bounds__(kAtJoin) void k_attend_join(AttendArgs a, int tile_
         __builtin_memcpy(&z, __builtin_assume_aligned(&so[w][d], 16), 32);
         v += z;
     }
-    write_row<T>(a, bh / a.c.heads, bh % a.c.heads, row, d, v);
+    const int b = a.heads_(bh);
+    write_row<T>(a, b, bh - b * a.c.heads, row, d, v);
 }
 
 // ---- host -----------------------------------------------------------------------
@@ -707,6 +706,10 @@ void attend_plan(AttendArgs& a, int precision) {
     s = s < by_room ? s : by_room;
     s = s < kAtMaxSplits ? s : kAtMaxSplits;
     a.splits = s < 2 ? 1 : (int)s;
+    a.splits_.by(a.splits);
+    a.tiles_.by((unsigned)((rows + 16 * nt - 1) / (16 * nt)));
+    a.heads_.by(a.c.heads);
+    a.group_.by(a.group);
     // a token each of sequences that may be of unequal lengths, and two
     // workgroups on most compute units
     const bool two = groups > kAtTarget && groups <= 2 * kAtTarget && bytes <= 256;
@@ -715,7 +718,7 @@ void attend_plan(AttendArgs& a, int precision) {
 
 template <int DP, class T, int NT>
 static void join(const AttendArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL((k_attend_join<DP, T>), dim3((unsigned)(a.B * a.c.heads * a.n * a.group)), dim3(kAtJoin), 0, st, a, 16 * NT);
+    hipLaunchKernelGGL((k_attend_join<DP, T, NT>), dim3(a.n * a.group, a.B * a.c.heads), dim3(kAtJoin), 0, st, a);
 }
 
 template <int DP, class T, int NT>

@@ -46,6 +46,20 @@ constexpr int kErrKvRange = 1, kErrKvPage = 2;
 // rows of partial results that a cache's workspace holds (see attend_plan)
 constexpr long long kAttendWorkRows = 1 << 16;
 
+// n / d for n < 2^31 by a product: with 2^l the power from d up, mul =
+// floor(2^(31 + l) / d) + 1 is off by less than 2^(31 + l) / (d n).  (The
+// compiler's own division is some 25 dependent instructions, and a short
+// call's kernels begin with four.)
+struct KvDiv {
+    unsigned mul;
+    int shift;
+    void by(unsigned d) {
+        for (shift = 31; d > 1ull << (shift - 31);) ++shift;
+        mul = (unsigned)((1ull << shift) / d + 1);
+    }
+    __device__ unsigned operator()(unsigned n) const { return (unsigned)((unsigned long long)n * mul >> shift); }
+};
+
 struct KvCache {                     // what the kernels need of a cache
     uint8_t* pool;
     int* err;
@@ -55,6 +69,41 @@ struct KvCache {                     // what the kernels need of a cache
     __host__ __device__ size_t head_bytes() const { return ((size_t)dp * 17 / 16) << page_shift; }
     __host__ __device__ size_t page_bytes() const { return head_bytes() * heads; }
 };
+
+// Reductions over lanes in registers (all 64 lanes active), where the exchange
+// by __shfl_xor waits for the LDS unit.  lanes16: over a row of 16, lanes64: over
+// the four rows too, lanes4: over four.
+template <int CTRL>
+__device__ __forceinline__ float lane_move(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+template <int CTRL>
+__device__ __forceinline__ int lane_move(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xf, 0xf, true); }
+
+template <class T, class F>
+__device__ __forceinline__ T lanes4(T x, F f) {
+    x = f(x, lane_move<0xb1>(x));        // quad_perm 1 0 3 2
+    return f(x, lane_move<0x4e>(x));     // quad_perm 2 3 0 1
+}
+template <class T, class F>
+__device__ __forceinline__ T lanes16(T x, F f) {
+    x = lanes4(x, f);
+    x = f(x, lane_move<0x124>(x));       // the quad before
+    return f(x, lane_move<0x128>(x));    // and the two before these
+}
+// over the four rows: f of both halves of a swap of x with itself
+template <class F>
+__device__ __forceinline__ float lane_rows(float x, F f) {
+    auto two = [&](const auto& r) {
+        const unsigned a = r[0], b = r[1];
+        return f(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+    };
+    unsigned u = __builtin_bit_cast(unsigned, x);
+    u = __builtin_bit_cast(unsigned, two(__builtin_amdgcn_permlane16_swap(u, u, false, false)));
+    return two(__builtin_amdgcn_permlane32_swap(u, u, false, false));
+}
+template <class F>
+__device__ __forceinline__ float lanes64(float x, F f) { return lane_rows(lanes16(x, f), f); }
 
 // Offsets in a record.
 template <int DP>
@@ -98,6 +147,7 @@ struct KvTokens {                    // the tokens a write or read takes
     const int *table, *first, *counts;
     int table_pages, B, n;
     int records;                     // of a sequence and head that n tokens may reach into
+    KvDiv heads_, records_;
 };
 
 struct AttendArgs {
@@ -110,6 +160,7 @@ struct AttendArgs {
     int max_visible, splits;
     int ahead;                       // > 0: sequences by length, this many from the longest down
     float scale_log2;                // scale * log2(e)
+    KvDiv splits_, tiles_, heads_, group_;   // tiles_: of rows
     float *part_o, *part_ml;         // partial results: channels, and (maximum, sum)
 };
 

@@ -26,7 +26,8 @@ struct KvWork {
 
 template <int DP>
 __device__ __forceinline__ KvWork kv_work(const KvCache& c, const KvTokens& a) {
-    const int head = blockIdx.x % c.heads, rec = blockIdx.x / c.heads % a.records, b = blockIdx.x / c.heads / a.records;
+    const int block = blockIdx.x, above = a.heads_(block), b = a.records_(above);
+    const int head = block - above * c.heads, rec = above - b * a.records;
     const int first = a.first[b], count = a.counts ? min(a.counts[b], a.n) : a.n;
     const long long at = (long long)(first >> 5) + rec;            // the record's place in the sequence
     KvWork w{nullptr, b, head, 0, at * kKvTile - first, count};
@@ -116,13 +117,12 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_write(KvCache c, KvRows k, Kv
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             // the bits of |x| order as the values do; a NaN's lie above infinity's
-            unsigned top = 0;
+            int top = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, __builtin_bit_cast(unsigned, x[s][j][e]) & 0x7fffffffu);
-            top = max(top, (unsigned)__shfl_xor((int)top, 1));
-            top = max(top, (unsigned)__shfl_xor((int)top, 2));
+            for (int e = 0; e < 8; ++e) top = max(top, __builtin_bit_cast(int, x[s][j][e]) & 0x7fffffff);
+            top = lanes4(top, [](int a, int b) { return max(a, b); });
             float inv;
-            power[s] = kv_power(top, inv);
+            power[s] = kv_power((unsigned)top, inv);
             code[s] = kv_code(x[s][j], inv);
         }
         uint8_t* at = o.record + L::value_at(t, w * 8);
@@ -281,7 +281,9 @@ static int kv_tokens(const Cache* c, int precision, int B, int n, const int32_t*
     // records that n tokens may reach into, wherever the first one lies
     const long long records = ((long long)n + 2 * (kKvTile - 1)) / kKvTile;
     if (B * records * c->c.heads >= 0x7fffffffLL) return fail(WF_E_UNSUPPORTED, "more than 2^31 records in one call");
-    *out = {table, first, counts, table_pages, B, n, (int)records};
+    *out = {table, first, counts, table_pages, B, n, (int)records, {}, {}};
+    out->heads_.by(c->c.heads);
+    out->records_.by((unsigned)records);
     return WF_OK;
 }
 
