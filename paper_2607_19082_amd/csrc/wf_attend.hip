@@ -330,40 +330,38 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     if constexpr (NT == 1)
         if (a.ahead) b = by_length(a, b, a.ahead);
 
-    // the lane's rows: their queries, and how many tokens they see
-    b8 q[NT][NK][NQ];
+    const SharedInts table = (SharedInts)(a.table + (size_t)b * a.table_pages);
+    const int in_page = a.c.page_shift - 5;
+    const uint8_t* pool = a.c.pool + (size_t)head * a.c.head_bytes();
+    const size_t page_bytes = a.c.page_bytes();
+
+    // What the rows see, their queries, and the page that the wave begins with
+    // if a row sees all it may: in flight together, since each waits as long as
+    // a short call's whole arithmetic takes.
+    const int expect = (a.splits_((a.max_visible + kKvTile - 1) / kKvTile + a.splits - 1) * split + wave) >> in_page;
+    const int expected = a.max_visible ? table[min(expect, a.table_pages - 1)] : 0;
     int see[NT], most = 0, least = a.max_visible;
+    T raw[NT][NK][8];
     const uint8_t* mask[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const int row = rt * 16 * NT + t * 16 + col;
-        const bool on = row < rows;
+        const bool on = row < rows;                    // a column past the last row repeats the first
         const int i = on ? a.group_(row) : 0, h = (head - i) * a.group + (on ? row : 0);
-        int s = on ? a.visible[(size_t)b * a.n + i] : 0;
-        if (s > a.max_visible) {
-            atomicOr(a.c.err, kErrKvRange);
-            s = a.max_visible;
-        }
-        see[t] = max(s, 0);
-        most = max(most, see[t]);
-        if (on) least = min(least, see[t]);
+        see[t] = a.visible[(size_t)b * a.n + i];
         mask[t] = MASK ? a.mask + b * a.mb + i * a.mr : nullptr;
         const T* p = (const T*)a.q.p + b * a.q.sb + i * a.q.sr + h * a.q.sh;
 #pragma unroll
-        for (int kk = 0; kk < NK; ++kk) {
-            const int d = DP / 4 * g + 8 * kk;
-            float x[8];
-            if (on && d + 8 <= a.c.dim) {
-                T r[8];
-                __builtin_memcpy(r, p + d, sizeof r);
+        for (int kk = 0; kk < NK; ++kk) __builtin_memcpy(raw[t][kk], p + min(DP / 4 * g + 8 * kk, a.c.dim - 8), sizeof raw[t][kk]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = (float)r[e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = 0.0f;
-            }
-            parts<NQ>(x, q[t][kk]);
-        }
+    for (int t = 0; t < NT; ++t) {
+        const bool on = rt * 16 * NT + t * 16 + col < rows;
+        if (on && see[t] > a.max_visible) atomicOr(a.c.err, kErrKvRange);
+        see[t] = on ? max(0, min(see[t], a.max_visible)) : 0;
+        most = max(most, see[t]);
+        if (on) least = min(least, see[t]);
     }
     most = __builtin_amdgcn_readfirstlane(lanes16(most, [](int x, int y) { return max(x, y); }));
     least = __builtin_amdgcn_readfirstlane(lanes16(least, [](int x, int y) { return min(x, y); }));
@@ -372,10 +370,26 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     const int tiles = (most + kKvTile - 1) / kKvTile;
     const int share = a.splits_(tiles + a.splits - 1);
     const int t0 = split * share, t1 = min(tiles, t0 + share);
-    const SharedInts table = (SharedInts)(a.table + (size_t)b * a.table_pages);
-    const int in_page = a.c.page_shift - 5;
-    const uint8_t* pool = a.c.pool + (size_t)head * a.c.head_bytes();
-    const size_t page_bytes = a.c.page_bytes();
+
+    b8 q[NT][NK][NQ];
+    auto make_queries = [&] {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int kk = 0; kk < NK; ++kk) {
+                const bool in = DP / 4 * g + 8 * kk < a.c.dim;
+                if constexpr (NQ == 1) {
+                    u4 w;
+                    __builtin_memcpy(&w, raw[t][kk], sizeof w);
+                    q[t][kk][0] = __builtin_bit_cast(b8, in ? w : u4{0, 0, 0, 0});
+                } else {
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = in ? (float)raw[t][kk][e] : 0.0f;
+                    parts<NQ>(x, q[t][kk]);
+                }
+            }
+    };
 
     f4 o[NT][ND], l[NT], bad[NT];
     // the row's maximum so far, and the score that raises it (none: 0 and
@@ -425,11 +439,13 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
             // a page outside the pool: its tokens are left out (another page's
             // are loaded in their place)
             auto inside = [&](int page) { return page >= 0 && page < a.c.pages; };
-            int page = page_of(tile0), next = page_of(tile0 + NW);
+            const int page = tile0 >> in_page == expect ? expected : page_of(tile0);
             bool there = inside(page), missing = !there;
             const uint8_t* record = record_of(tile0, there ? page : 0);
             load_keys(keys, record, lane);
             if constexpr (MASK) load_mask(tile0);
+            int next = page_of(tile0 + NW);
+            if constexpr (!kCareful) make_queries();
             // The next tile's keys are loaded as soon as this one's are used
             // up, its values then, and the page of the one after it.  Past
             // the end it is the last tile again, so that the loads in flight
