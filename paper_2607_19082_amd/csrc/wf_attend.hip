@@ -712,11 +712,14 @@ void attend_plan(AttendArgs& a, int precision) {
     const int bytes = a.c.dp * (precision == WF_BF16 ? 2 : 4), nt = row_tiles(a, precision), rows = a.n * a.group;
     const int waves = nt == 1 && bytes < 1024 ? 8 : 4;
     const long long groups = (long long)a.B * a.c.heads * ((rows + 16 * nt - 1) / (16 * nt));
-    // at least four tiles for each wave, below which the join costs more than
-    // the split gains (68 masked rows over 8101 tokens: 16.4 us with one, 17.0
-    // with four, 18.4 with six; a token over 1001 10.2 with one, 9.1)
+    // A tile takes a wave about 1 us and the join 3, so up to four tiles a wave
+    // are not split; more are, down to one tile each.  us with no split, four
+    // tiles each, two and one: a token over 1001 (8 heads of 128, bf16) 7.8, 7.8,
+    // 8.6, 7.8, over 2047 11.4, 10.5, 8.6, 7.9, over 8192 33, 10.7, 9.2, 8.6; 45
+    // fp32 rows over 1024 7.1, 7.2, 8.6, 8.0, over 4096 15.5, 10.2, 8.8, 8.5.
+    const long long tiles = ((long long)a.max_visible + kKvTile - 1) / kKvTile;
+    const long long by_len = tiles <= 4 * waves ? 1 : (tiles + waves - 1) / waves;
     long long s = kAtTarget / groups;
-    const long long by_len = a.max_visible / (4 * waves * kKvTile);
     s = s < by_len ? s : by_len;
     const long long by_room = kAttendWorkRows / (groups * 16 * nt);
     s = s < by_room ? s : by_room;
