@@ -477,7 +477,9 @@ class Cache:
         self._device = torch.cuda.current_device()
         self.heads, self.dim, self.pages, self.page = heads, dim, pages, page
         # a serving step makes several short calls: what they look up is kept
-        self._lib, self._torch = lib(), torch
+        self._lib = lib()
+        self._int, self._float, self._bool, self._empty, self._empty_like = \
+            torch.int32, torch.float32, torch.bool, torch.empty, torch.empty_like
         self._precision = {torch.float32: 0, torch.bfloat16: 1}
         # the handle of a device's current stream, without a Stream object
         self._current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
@@ -495,17 +497,18 @@ class Cache:
             pass
 
     def _rows(self, t, shape, dtype, name):
-        if t.get_device() != self._device or t.dtype != dtype or t.shape != shape or (t.stride(3) != 1 and t.numel()):
-            raise ValueError(f"{name}: expected a {dtype} tensor {tuple(shape)} on device {self._device} with contiguous "
-                             f"channels, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
-        sequence, token, head, _ = t.stride()
-        return _pack_rows(t.data_ptr(), sequence, token, head)
+        if t.dtype is dtype and t.shape == shape and t.get_device() == self._device:
+            sequence, token, head, channel = t.stride()
+            if channel == 1 or not t.numel():
+                return _pack_rows(t.data_ptr(), sequence, token, head)
+        raise ValueError(f"{name}: expected a {dtype} tensor {tuple(shape)} on device {self._device} with contiguous "
+                         f"channels, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
 
     def _ints(self, t, shape, name):
-        if t.get_device() != self._device or t.dtype != self._torch.int32 or t.shape != shape or not t.is_contiguous():
-            raise ValueError(f"{name}: expected a contiguous int32 tensor {tuple(shape)} on device {self._device}, got "
-                             f"{t.dtype} {tuple(t.shape)} on {t.device}")
-        return t.data_ptr()
+        if t.dtype is self._int and t.shape == shape and t.get_device() == self._device and t.is_contiguous():
+            return t.data_ptr()
+        raise ValueError(f"{name}: expected a contiguous int32 tensor {tuple(shape)} on device {self._device}, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
 
     def _type(self, dtype):
         precision = self._precision.get(dtype)
@@ -514,32 +517,35 @@ class Cache:
         return precision
 
     def _table(self, table, B):
-        if table.dim() != 2:
-            raise ValueError(f"table: expected two dimensions, got {tuple(table.shape)}")
-        pages = table.shape[1]
-        return self._ints(table, (B, pages), "table"), pages
+        shape = table.shape
+        if len(shape) != 2:
+            raise ValueError(f"table: expected two dimensions, got {tuple(shape)}")
+        return self._ints(table, (B, shape[1]), "table"), shape[1]
 
-    def _empty(self, shape, dtype, device, stream, like=None):
-        t = self._torch.empty(shape, dtype=dtype, device=device) if like is None else self._torch.empty_like(like)
+    def _new(self, shape, dtype, stream, like=None):
+        """A contiguous tensor and its rows."""
+        t = self._empty(shape, dtype=dtype, device=self._device) if like is None else self._empty_like(like)
         if stream is not None:          # allocated on the current stream, used on another
             t.record_stream(stream)
-        return t
+        _, n, heads, dim = shape
+        return t, _pack_rows(t.data_ptr(), n * heads * dim, heads * dim, dim)
 
-    def _stream(self, stream, device):
-        return self._current(device.index) if stream is None else stream.cuda_stream
+    def _stream(self, stream):
+        return self._current(self._device) if stream is None else stream.cuda_stream
 
     def write(self, k, v, table, first, counts=None, stream=None):
         """Quantise k and v [B][n][heads][dim] into the cache: token i of
         sequence b at position first[b] + i, where i < counts[b] (None: all)."""
-        if k.dim() != 4:
-            raise ValueError(f"k: expected four dimensions, got {tuple(k.shape)}")
-        B, n = k.shape[:2]
-        shape, dtype = (B, n, self.heads, self.dim), k.dtype
+        shape, dtype = k.shape, k.dtype
+        if len(shape) != 4:
+            raise ValueError(f"k: expected four dimensions, got {tuple(shape)}")
+        B, n = shape[0], shape[1]
+        shape = (B, n, self.heads, self.dim)
         p_table, pages = self._table(table, B)
         rc = self._lib.wf_cache_write(
             self._h, self._type(dtype), self._rows(k, shape, dtype, "k"), self._rows(v, shape, dtype, "v"), B, n, p_table,
             pages, self._ints(first, (B,), "first"), None if counts is None else self._ints(counts, (B,), "counts"),
-            self._stream(stream, k.device))
+            self._stream(stream))
         if rc:
             _check(rc)
 
@@ -551,16 +557,18 @@ class Cache:
         p_table, pages = self._table(table, B)
         shape = (B, n, self.heads, self.dim)
         if out is None:
-            dtype = self._torch.float32 if dtype is None else dtype
-            k = self._empty(shape, dtype, table.device, stream)
-            v = self._empty(shape, dtype, table.device, stream, like=k)
+            dtype = self._float if dtype is None else dtype
+            precision = self._type(dtype)
+            k, k_rows = self._new(shape, dtype, stream)
+            v, v_rows = self._new(shape, dtype, stream, like=k)
         else:
             k, v = out
             dtype = k.dtype
+            precision = self._type(dtype)
+            k_rows, v_rows = self._rows(k, shape, dtype, "k"), self._rows(v, shape, dtype, "v")
         rc = self._lib.wf_cache_read(
-            self._h, self._type(dtype), self._rows(k, shape, dtype, "k"), self._rows(v, shape, dtype, "v"), B, n, p_table,
-            pages, self._ints(first, (B,), "first"), None if counts is None else self._ints(counts, (B,), "counts"),
-            self._stream(stream, table.device))
+            self._h, precision, k_rows, v_rows, B, n, p_table, pages, self._ints(first, (B,), "first"),
+            None if counts is None else self._ints(counts, (B,), "counts"), self._stream(stream))
         if rc:
             _check(rc)
         return k, v
@@ -573,27 +581,30 @@ class Cache:
         the cache's heads; scale defaults to dim ** -0.5.  max_visible bounds
         visible (default: the mask's width, or all that the table holds; a
         tighter bound makes a better launch)."""
-        if q.dim() != 4:
-            raise ValueError(f"q: expected four dimensions, got {tuple(q.shape)}")
-        B, n, hq = q.shape[:3]
-        shape, dtype = (B, n, hq, self.dim), q.dtype
+        shape, dtype = q.shape, q.dtype
+        if len(shape) != 4:
+            raise ValueError(f"q: expected four dimensions, got {tuple(shape)}")
+        B, n, hq, _ = shape
+        shape, precision = (B, n, hq, self.dim), self._type(dtype)
+        q_rows = self._rows(q, shape, dtype, "q")
         p_table, pages = self._table(table, B)
         if max_visible is None:
             max_visible = pages * self.page if mask is None else mask.shape[-1]
         if out is None:
-            out = self._empty(shape, dtype, q.device, stream, like=q if q.is_contiguous() else None)
+            out, out_rows = self._new(shape, dtype, stream, like=q if q.is_contiguous() else None)
+        else:
+            out_rows = self._rows(out, shape, dtype, "out")
         p_mask = strides = None
         if mask is not None:
-            if mask.get_device() != self._device or mask.dtype != self._torch.bool or mask.shape != (B, n, max_visible) or \
+            if mask.get_device() != self._device or mask.dtype != self._bool or mask.shape != (B, n, max_visible) or \
                     (max_visible > 1 and mask.stride(2) != 1):
                 raise ValueError(f"mask: expected a bool tensor {(B, n, max_visible)} on device {self._device} with "
                                  f"contiguous tokens, got {mask.dtype} {tuple(mask.shape)}, strides {mask.stride()}, on "
                                  f"{mask.device}")
             p_mask, strides = mask.data_ptr(), (ctypes.c_int64 * 2)(mask.stride(0), mask.stride(1))
         rc = self._lib.wf_cache_attend(
-            self._h, self._type(dtype), self._rows(q, shape, dtype, "q"), self._rows(out, shape, dtype, "out"), B, n, hq,
-            p_table, pages, self._ints(visible, (B, n), "visible"), p_mask, strides, max_visible,
-            self.dim ** -0.5 if scale is None else scale, self._stream(stream, q.device))
+            self._h, precision, q_rows, out_rows, B, n, hq, p_table, pages, self._ints(visible, (B, n), "visible"),
+            p_mask, strides, max_visible, self.dim ** -0.5 if scale is None else scale, self._stream(stream))
         if rc:
             _check(rc)
         return out
