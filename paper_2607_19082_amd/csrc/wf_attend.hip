@@ -26,12 +26,13 @@
 // results.
 //
 // What bounds it (8 heads of 128, bf16, MI355X): a token each of 32 sequences
-// of 8192 tokens, 4 query heads a key head, takes 57 us for 286 MB, 5.0 TB/s
+// of 8192 tokens, 4 query heads a key head, takes 56 us for 286 MB, 5.1 TB/s
 // where a kernel that only reads reaches 5.7.  A tile costs a wave ~170 vector
 // instructions, 96 of them conversions and the exchange of values between
 // tokens, and 26 products; the two hardly overlap, so with many rows (1024
-// queries, 32 heads, 16384 tokens: 380 us, 0.70 PFLOP/s) their sum is the time,
-// and with few tokens a wave (1001 in all: 9 us) the chain of one tile is.
+// queries, 32 heads, 16384 tokens: 343 us, 0.78 PFLOP/s) their sum is the time.
+// A short call (a token over 1001: 8 us) is 4 us of launch, loads that wait for
+// each other and the join of the waves, and 1 for each tile of a wave.
 #include <cmath>
 #include <type_traits>
 
@@ -52,14 +53,15 @@ typedef unsigned u2 __attribute__((ext_vector_type(2)));
 typedef const int __attribute__((address_space(4))) * SharedInts;
 
 // Workgroups that a call is split into: one for each compute unit.  us for 192
-// / 256 / 320 / 512: one token over 131072 36 / 35 / 42 / 36; 45 fp32 rows over
-// 32300 19 / 17 / 21 / 18; 56 fp32 rows of 256 channels over 20011 30 / 26 / 38
-// / 34 (the last ones wait for a place, and the join has more to read).
+// / 256 / 320 / 512: one token over 131072 35 / 33 / 40 / 34; 45 fp32 rows over
+// 32300 17 / 14 / 19 / 16; 56 fp32 rows of 256 channels over 20011 28 / 24 / 34
+// / 30 (the last ones wait for a place, and the join has more to read).
 constexpr int kAtTarget = 256;
 constexpr int kAtMaxSplits = 256;
 constexpr int kAtJoin = 256;        // threads of the kernel that joins the splits
-// Waves of a workgroup.  (16 instead of 8: 10.2 against 9.1 us for a token over
-// 1001, since the larger workgroup starts later.)
+// Waves of a workgroup.  (16 instead of 8: 9.0 against 8.1 us for a token over
+// 1001, 16 against 14.4 for 45 fp32 rows over 32300, since the larger workgroup
+// starts later.)
 template <int DP, class T, int NT>
 constexpr int kAtWaves = NT == 1 && DP * sizeof(T) < 1024 ? 8 : 4;
 // a row's maximum is raised only when a score passes it by this much (in
@@ -295,7 +297,8 @@ constexpr int kAtBatch = 256;       // sequences that are taken by length, at mo
 // The sequence that holds a place among all, from the longest down and, past
 // the first `ahead` places, from the shortest up: workgroups of the two halves
 // share a compute unit, and each then has about the same to do.  64 sequences
-// of 0 to 8192 tokens, 8 heads of 128: 62 us, in the order given 70.
+// of 0 to 8192 tokens, 8 heads of 128: 60 us, in the order given 67 (of 8192
+// tokens each 110 and 106).
 __device__ __forceinline__ int by_length(const AttendArgs& a, int place, int ahead) {
     __shared__ int length[kAtBatch], found;
     const int u = threadIdx.x;
@@ -694,10 +697,10 @@ __global__ __launch_bounds__(kAtJoin) void k_attend_join(AttendArgs a) {
 
 // Column tiles of a workgroup: two, which share a tile's conversions, where they
 // fit the registers and there are enough rows to fill the chip all the same.
-// us with one / two, 8 heads, 8192 tokens: of 128 in bf16, 256 tiles of rows 40
-// / 46, 512 72 / 65, 1024 135 / 110, 2048 248 / 203; of 64 in bf16, 512 48 /
-// 50, 768 69 / 74, 1024 85 / 74; of 64 in fp32, 512 58 / 57, 768 80 / 86, 1024
-// 102 / 91.  Hence tiles times channels.
+// us with one / two, 8 heads, 8192 tokens: of 128 in bf16, 256 tiles of rows 41
+// / 43, 512 73 / 66, 1024 136 / 111, 2048 262 / 210; of 64 in bf16, 512 50 /
+// 51, 768 70 / 76, 1024 91 / 79; of 64 in fp32, 512 58 / 56, 768 83 / 89, 1024
+// 107 / 94.  Hence tiles times channels.
 template <int DP, class T>
 constexpr bool kAtTwoTiles = DP * sizeof(T) <= 256;
 constexpr long long kAtManyRows = 1 << 16;
