@@ -114,8 +114,9 @@ __device__ __forceinline__ void parts(const float (&x)[8], h8 (&p)[N]) {
 // the other pair.
 template <int N>
 __device__ __forceinline__ void parts(const float (&x)[8], b8 (&p)[N]) {
-    unsigned first = 0x0000bf80u, second = 0xbf800000u;
-    asm("" : "+s"(first), "+s"(second));
+    unsigned first, second;
+    asm("s_mov_b32 %0, 0xbf80" : "=s"(first));
+    asm("s_mov_b32 %0, 0xbf800000" : "=s"(second));
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
         f2 r = {x[e], x[e + 1]};
