@@ -488,9 +488,10 @@ void wf_xform_destroy(wf_xform_t plan);
  * block of a head may be shorter) holds 4-bit values {0, 1/2, 1, 3/2, 2, 3, 4,
  * 6} with a sign, times 2^e: e is the least integer in [-125, 125] with
  * 6 * 2^e >= the block's largest magnitude, so that nothing is cut off, and
- * x / 2^e is rounded to the nearest value, a tie to the even code (magnitudes beyond 6 * 2^125 are held
- * as that).  A block with a value that is not finite reads back as NaN.  4.25
- * bits a value; the bytes' order in a page is the library's own.
+ * x / 2^e is rounded to the nearest value, a tie to the even code (magnitudes
+ * beyond 6 * 2^125 are held as that).  A block with a value that is not finite
+ * reads back as NaN.  4.25 bits a value; the bytes' order in a page is the
+ * library's own.
  *
  * Tokens lie in pages: token t of sequence b is in page
  * table[b][t / page] of the pool, at place t % page.
@@ -528,6 +529,8 @@ int wf_cache_plan(const wf_cache_desc *desc, wf_cache_t *out);
  * A token past the table, or in a page outside the pool, is not written, and
  * the next wf_cache_sync returns WF_E_CAPACITY or WF_E_INVALID.  Two tokens of
  * one call at one place are a race.  Asynchronous on `stream`.
+ * Errors: WF_E_INVALID; WF_E_UNSUPPORTED where B * heads * (n + 62) / 32 is 2^24
+ * or more.
  */
 int wf_cache_write(wf_cache_t cache, int32_t precision, const wf_rows *k, const wf_rows *v, int32_t B, int32_t n,
                    const int32_t *table, int32_t table_pages, const int32_t *first, const int32_t *counts,
@@ -561,8 +564,10 @@ int wf_cache_read(wf_cache_t cache, int32_t precision, const wf_rows *k, const w
  * Tokens in a page outside the pool are left out, and the next wf_cache_sync
  * returns WF_E_INVALID.  Sums are held in fp32, before they are divided (they
  * overflow where |v| is beyond about 2^112 / the row's tokens), and their order
- * depends on the call's sizes alone.  Asynchronous on `stream`; one call in flight per cache
- * (the workspace is shared by its calls).
+ * depends on the call's sizes alone.  Asynchronous on `stream`; one call in
+ * flight per cache (the workspace is shared by its calls).
+ * Errors: WF_E_INVALID; WF_E_UNSUPPORTED for a call of 2^23 workgroups of 16
+ * rows or more.
  */
 int wf_cache_attend(wf_cache_t cache, int32_t precision, const wf_rows *q, const wf_rows *out, int32_t B, int32_t n,
                     int32_t q_heads, const int32_t *table, int32_t table_pages, const int32_t *visible,

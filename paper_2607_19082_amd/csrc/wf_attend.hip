@@ -712,7 +712,7 @@ static int row_tiles(const AttendArgs& a, int precision) {
     return rows > 16 && tiles * a.c.dp >= kAtManyRows && a.c.dp * (precision == WF_BF16 ? 2 : 4) <= 256 ? 2 : 1;
 }
 
-void attend_plan(AttendArgs& a, int precision) {
+long long attend_plan(AttendArgs& a, int precision) {
     const int bytes = a.c.dp * (precision == WF_BF16 ? 2 : 4), nt = row_tiles(a, precision), rows = a.n * a.group;
     const int waves = nt == 1 && bytes < 1024 ? 8 : 4;
     const long long groups = (long long)a.B * a.c.heads * ((rows + 16 * nt - 1) / (16 * nt));
@@ -737,6 +737,7 @@ void attend_plan(AttendArgs& a, int precision) {
     // workgroups on most compute units
     const bool two = groups > kAtTarget && groups <= 2 * kAtTarget && bytes <= 256;
     a.ahead = nt == 1 && rows <= 16 && a.B > 1 && a.B <= kAtBatch && two ? (int)(kAtTarget / a.c.heads) : 0;
+    return groups * a.splits * waves * 64;
 }
 
 template <int DP, class T, int NT>

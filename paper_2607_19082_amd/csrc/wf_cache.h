@@ -166,8 +166,9 @@ struct AttendArgs {
 
 void launch_kv_write(const KvCache&, int precision, const KvRows& k, const KvRows& v, const KvTokens&, hipStream_t);
 void launch_kv_read(const KvCache&, int precision, const KvRows& k, const KvRows& v, const KvTokens&, hipStream_t);
-// The splits of a call, so that its partial results fit the workspace.
-void attend_plan(AttendArgs&, int precision);
+// The splits of a call, so that its partial results fit the workspace.  Returns
+// the threads of its launch.
+long long attend_plan(AttendArgs&, int precision);
 void launch_attend(const AttendArgs&, int precision, hipStream_t);
 
 }  // namespace wf

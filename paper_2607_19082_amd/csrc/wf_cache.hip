@@ -280,7 +280,7 @@ static int kv_tokens(const Cache* c, int precision, int B, int n, const int32_t*
     if (B && n && (!table || !first)) return fail(WF_E_INVALID, "table or first is NULL");
     // records that n tokens may reach into, wherever the first one lies
     const long long records = ((long long)n + 2 * (kKvTile - 1)) / kKvTile;
-    if (B * records * c->c.heads >= 0x7fffffffLL) return fail(WF_E_UNSUPPORTED, "more than 2^31 records in one call");
+    if (B * records * c->c.heads * kKvThreads >= 1LL << 32) return fail(WF_E_UNSUPPORTED, "2^24 or more records in one call");
     *out = {table, first, counts, table_pages, B, n, (int)records, {}, {}};
     out->heads_.by(c->c.heads);
     out->records_.by((unsigned)records);
@@ -298,7 +298,9 @@ using namespace wf;
 
 extern "C" {
 
-int wf_cache_plan(const wf_cache_desc* d, wf_cache_t* out) {
+// (a message that cannot be built is the one thing that throws in these)
+
+int wf_cache_plan(const wf_cache_desc* d, wf_cache_t* out) try {
     if (!out) return fail(WF_E_INVALID, "out is NULL");
     *out = nullptr;
     if (!d) return fail(WF_E_INVALID, "desc is NULL");
@@ -335,12 +337,14 @@ int wf_cache_plan(const wf_cache_desc* d, wf_cache_t* out) {
     }
     *out = reinterpret_cast<wf_cache_t>(c);
     return WF_OK;
+} catch (...) {
+    return WF_E_NOMEM;
 }
 
 void wf_cache_destroy(wf_cache_t cache) { free_cache(reinterpret_cast<Cache*>(cache)); }
 
 int wf_cache_write(wf_cache_t cache, int32_t precision, const wf_rows* k, const wf_rows* v, int32_t B, int32_t n,
-                   const int32_t* table, int32_t table_pages, const int32_t* first, const int32_t* counts, hipStream_t stream) {
+                   const int32_t* table, int32_t table_pages, const int32_t* first, const int32_t* counts, hipStream_t stream) try {
     const Cache* c = reinterpret_cast<Cache*>(cache);
     KvTokens a;
     KvRows kr, vr;
@@ -349,10 +353,12 @@ int wf_cache_write(wf_cache_t cache, int32_t precision, const wf_rows* k, const 
     if ((rc = kv_rows(k, precision, "k", &kr)) != WF_OK || (rc = kv_rows(v, precision, "v", &vr)) != WF_OK) return rc;
     launch_kv_write(c->c, precision, kr, vr, a, stream);
     return kv_launched("wf_cache_write");
+} catch (...) {
+    return WF_E_NOMEM;
 }
 
 int wf_cache_read(wf_cache_t cache, int32_t precision, const wf_rows* k, const wf_rows* v, int32_t B, int32_t n,
-                  const int32_t* table, int32_t table_pages, const int32_t* first, const int32_t* counts, hipStream_t stream) {
+                  const int32_t* table, int32_t table_pages, const int32_t* first, const int32_t* counts, hipStream_t stream) try {
     const Cache* c = reinterpret_cast<Cache*>(cache);
     KvTokens a;
     KvRows kr, vr;
@@ -361,11 +367,13 @@ int wf_cache_read(wf_cache_t cache, int32_t precision, const wf_rows* k, const w
     if ((rc = kv_rows(k, precision, "k", &kr)) != WF_OK || (rc = kv_rows(v, precision, "v", &vr)) != WF_OK) return rc;
     launch_kv_read(c->c, precision, kr, vr, a, stream);
     return kv_launched("wf_cache_read");
+} catch (...) {
+    return WF_E_NOMEM;
 }
 
 int wf_cache_attend(wf_cache_t cache, int32_t precision, const wf_rows* q, const wf_rows* out, int32_t B, int32_t n,
                     int32_t q_heads, const int32_t* table, int32_t table_pages, const int32_t* visible,
-                    const uint8_t* mask, const int64_t* mask_stride, int32_t max_visible, float scale, hipStream_t stream) {
+                    const uint8_t* mask, const int64_t* mask_stride, int32_t max_visible, float scale, hipStream_t stream) try {
     const Cache* c = reinterpret_cast<Cache*>(cache);
     if (!c) return fail(WF_E_INVALID, "cache is NULL");
     if (precision != WF_FP32 && precision != WF_BF16) return fail(WF_E_INVALID, "unknown precision");
@@ -388,14 +396,16 @@ int wf_cache_attend(wf_cache_t cache, int32_t precision, const wf_rows* q, const
     a.table_pages = table_pages; a.B = B; a.n = n; a.group = q_heads / c->c.heads;
     a.max_visible = max_visible;
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
-    attend_plan(a, precision);
+    if (attend_plan(a, precision) >= 1LL << 32) return fail(WF_E_UNSUPPORTED, "2^32 or more threads in one call");
     a.part_o = c->work;
     a.part_ml = c->work + (size_t)kAttendWorkRows * c->c.dp;
     launch_attend(a, precision, stream);
     return kv_launched("wf_cache_attend");
+} catch (...) {
+    return WF_E_NOMEM;
 }
 
-int wf_cache_sync(wf_cache_t cache, hipStream_t stream) {
+int wf_cache_sync(wf_cache_t cache, hipStream_t stream) try {
     Cache* c = reinterpret_cast<Cache*>(cache);
     if (!c) return fail(WF_E_INVALID, "cache is NULL");
     int err = 0;
@@ -406,6 +416,8 @@ int wf_cache_sync(wf_cache_t cache, hipStream_t stream) {
     if (err & kErrKvPage) return fail(WF_E_INVALID, "a page table entry lies outside the pool");
     if (err & kErrKvRange) return fail(WF_E_CAPACITY, "a token lies past its page table, or a row sees more than max_visible tokens");
     return WF_OK;
+} catch (...) {
+    return WF_E_NOMEM;
 }
 
 }  // extern "C"

@@ -552,3 +552,21 @@ def test_a_pool_that_does_not_fit():
     assert torch.equal(c.read(table, ints([0]), 40)[0][0].cpu(), torch.from_numpy(oracle.quantise(k[0].numpy())).float())
     c.sync()
     c.close()
+
+
+def test_a_launch_that_is_too_large():
+    c = wf.Cache(1, 8, 1)
+    B = 1 << 23                                     # workgroups of 512 threads
+    q = torch.zeros((B, 1, 1, 8), dtype=torch.bfloat16, device="cuda")
+    table, visible = torch.empty((B, 0), dtype=torch.int32, device="cuda"), torch.zeros((B, 1), dtype=torch.int32, device="cuda")
+    with pytest.raises(wf.WfError) as e:
+        c.attend(q, table, visible)
+    assert e.value.code == wf.WF_E_UNSUPPORTED
+    many = q.expand(B, 40, 1, 8)                    # which may reach into three records
+    with pytest.raises(wf.WfError) as e:
+        c.write(many, many, visible, visible[:, 0].contiguous())
+    assert e.value.code == wf.WF_E_UNSUPPORTED
+    half = slice(0, B // 2)
+    assert (c.attend(q[half] + 1, table[half], visible[half]) == 0).all()
+    c.sync()
+    c.close()
