@@ -724,6 +724,13 @@ long long attend_plan(AttendArgs& a, int precision) {
     const long long tiles = ((long long)a.max_visible + kKvTile - 1) / kKvTile;
     const long long by_len = tiles <= 4 * waves ? 1 : (tiles + waves - 1) / waves;
     long long s = kAtTarget / groups;
+    // A few workgroups more than compute units would take as long as two each:
+    // where they are long, they are split into four.  us without and with, 33
+    // tokens over 4096 46 / 40, 8192 83 / 69, 16384 155 / 120, 40 over 8192 86 /
+    // 75, 44 86 / 82; 320 tiles of rows over 4096 37 / 41, 8192 65 / 56, 16384 116
+    // / 90; of 64 channels in fp32 30 / 36, 52 / 50, 91 / 72; 36 tokens over 0 to
+    // 8192 47 / 49, 0 to 16384 88 / 81.
+    if (groups > kAtTarget && groups <= kAtTarget * 5 / 4 && tiles >= 256) s = 4;
     s = s < by_len ? s : by_len;
     const long long by_room = kAttendWorkRows / (groups * 16 * nt);
     s = s < by_room ? s : by_room;
@@ -735,7 +742,7 @@ long long attend_plan(AttendArgs& a, int precision) {
     a.group_.by(a.group);
     // a token each of sequences that may be of unequal lengths, and two
     // workgroups on most compute units
-    const bool two = groups > kAtTarget && groups <= 2 * kAtTarget && bytes <= 256;
+    const bool two = groups > kAtTarget && groups <= 2 * kAtTarget && bytes <= 256 && a.splits == 1;
     a.ahead = nt == 1 && rows <= 16 && a.B > 1 && a.B <= kAtBatch && two ? (int)(kAtTarget / a.c.heads) : 0;
     return groups * a.splits * waves * 64;
 }

@@ -370,6 +370,21 @@ def test_rows_that_fill_the_chip(dim, n, group, heads, B, dtype, masked):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("heads,n,lens", [(260, 1, [8200]), (130, 2, [8193, 5000]), (64, 3, [8200, 0, 31, 2047, 1])])
+def test_a_few_more_than_compute_units(heads, n, lens, dtype):
+    """Long calls of 257 to 320 workgroups, which are split."""
+    B, L = len(lens), max(lens)
+    k, v = draw((B, L, heads, 8), dtype, 1), draw((B, L, heads, 8), dtype, 2)
+    q = draw((B, n, heads, 8), dtype, 3, 0.0)
+    vis = [[max(0, x - i) for i in range(n)] for x in lens]
+    c, table = filled(k, v, page=256)
+    out = c.attend(q.cuda(), table, ints(vis), max_visible=L)
+    c.sync()
+    check(out, q, oracle.quantise(k.float().numpy()), oracle.quantise(v.float().numpy()), vis, dtype)
+    c.close()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("dim,n,group,L", [(64, 1, 2, 300), (128, 3, 1, 600), (256, 1, 1, 90), (128, 400, 4, 70)])
 def test_values_of_any_size(dim, n, group, L, dtype):
     """Values from 2^-100 to 2^100, in one channel or from token to token; the
