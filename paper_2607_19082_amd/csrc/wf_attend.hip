@@ -724,13 +724,20 @@ long long attend_plan(AttendArgs& a, int precision) {
     const long long tiles = ((long long)a.max_visible + kKvTile - 1) / kKvTile;
     const long long by_len = tiles <= 4 * waves ? 1 : (tiles + waves - 1) / waves;
     long long s = kAtTarget / groups;
-    // A few workgroups more than compute units would take as long as two each:
-    // where they are long, they are split into four.  us without and with, 33
-    // tokens over 4096 46 / 40, 8192 83 / 69, 16384 155 / 120, 40 over 8192 86 /
-    // 75, 44 86 / 82; 320 tiles of rows over 4096 37 / 41, 8192 65 / 56, 16384 116
-    // / 90; of 64 channels in fp32 30 / 36, 52 / 50, 91 / 72; 36 tokens over 0 to
-    // 8192 47 / 49, 0 to 16384 88 / 81.
-    if (groups > kAtTarget && groups <= kAtTarget * 5 / 4 && tiles >= 256) s = 4;
+    // Long calls (8192 tokens) that would leave many compute units idle take two
+    // workgroups each where that fills a fifth more: us without and with, 8 key
+    // heads of 128 in bf16, 17 tokens 44 / 38, 11 28 / 25, 18 over 0 to 8192 38 /
+    // 28, 136 tiles of rows 38 / 34; at 4096 tokens 23 / 22, 17 / 17, at 2048
+    // 13.5 / 16.  A few workgroups more than compute units would take as long as
+    // two each, and are split into four: 33 tokens over 4096 46 / 40, 8192 83 /
+    // 69, 16384 155 / 120, 40 over 8192 86 / 75, 44 86 / 82; 320 tiles of rows
+    // over 4096 37 / 41, 8192 65 / 56, 16384 116 / 90; of 64 channels in fp32 30 /
+    // 36, 52 / 50, 91 / 72; 36 tokens over 0 to 8192 47 / 49, 0 to 16384 88 / 81.
+    if (tiles >= 256) {
+        const long long twice = 2 * kAtTarget / groups;
+        if (s && 5 * twice > 12 * s) s = twice;
+        if (!s && groups <= kAtTarget * 5 / 4) s = 4;
+    }
     s = s < by_len ? s : by_len;
     const long long by_room = kAttendWorkRows / (groups * 16 * nt);
     s = s < by_room ? s : by_room;

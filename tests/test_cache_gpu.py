@@ -370,9 +370,11 @@ def test_rows_that_fill_the_chip(dim, n, group, heads, B, dtype, masked):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
-@pytest.mark.parametrize("heads,n,lens", [(260, 1, [8200]), (130, 2, [8193, 5000]), (64, 3, [8200, 0, 31, 2047, 1])])
+@pytest.mark.parametrize("heads,n,lens", [(260, 1, [8200]), (130, 2, [8193, 5000]), (64, 3, [8200, 0, 31, 2047, 1]),
+                                          (45, 5, [8200, 0, 3000]), (88, 17, [8170])])
 def test_a_few_more_than_compute_units(heads, n, lens, dtype):
-    """Long calls of 257 to 320 workgroups, which are split."""
+    """Long calls whose workgroups would fill the compute units badly: 257 to
+    320, or a half to five eighths of them (or of a part of them), are split."""
     B, L = len(lens), max(lens)
     k, v = draw((B, L, heads, 8), dtype, 1), draw((B, L, heads, 8), dtype, 2)
     q = draw((B, n, heads, 8), dtype, 3, 0.0)
