@@ -16,10 +16,12 @@
 // Operands: keys and values are exact in bf16.  bf16 queries are too; fp32
 // queries are three bf16 parts (24 bits).  Probabilities are two bf16 parts
 // (16 bits) for bf16 calls, so that the output's own rounding is the only one
-// that shows.  For fp32 calls they are two parts in half precision (22 bits),
-// with values in half precision too, where the values' powers allow that, and
-// three bf16 parts otherwise.  Scores, maxima, sums and outputs are held in
-// fp32; a row's sum is that of its rounded probabilities.
+// that shows, and three (24 bits) for fp32 calls.  bf16 has fp32's range, so a
+// probability keeps these bits however far it lies below the row's largest:
+// where the tokens that weigh most hold zeros in a channel, the small ones are
+// all that the channel has.  (Half precision takes 22 bits in two parts, but
+// ends at 2^-24.)  Scores, maxima, sums and outputs are held in fp32; a row's
+// sum is that of its rounded probabilities.
 //
 // The waves of a workgroup share the tokens and join at the end; with few rows
 // the tokens are also split over workgroups, and a second kernel joins their
@@ -42,8 +44,6 @@ namespace wf {
 
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
-typedef _Float16 h8 __attribute__((ext_vector_type(8)));
-typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef float f8 __attribute__((ext_vector_type(8)));
 typedef float f2 __attribute__((ext_vector_type(2)));
 typedef __bf16 b2 __attribute__((ext_vector_type(2)));
@@ -67,46 +67,24 @@ constexpr int kAtWaves = NT == 1 && DP * sizeof(T) < 1024 ? 8 : 4;
 // a row's maximum is raised only when a score passes it by this much (in
 // powers of two): its probabilities then stay below 2^8
 constexpr float kAtSlack = 8.0f;
-// Probabilities are held times 2^7, so that half precision takes them up to
-// that (2^15) and loses none above 2^-32 of the row's largest; the sums that
+// Probabilities are held times 2^7, so that the third part (2^-24 of the
+// first) is a normal number down to 2^-109 of the row's largest; the sums that
 // divide them are too.
 constexpr float kAtLift = 7.0f;
-// Power bytes 109 to 140 (2^-18 to 2^13): all values that they scale are exact
-// in half precision.
-constexpr unsigned kAtWindow = 0x6d6d6d6du;
 
-// parts of queries (bf16), of probabilities in half precision, and in bf16
+// bf16 parts of queries and of probabilities
 template <class T>
 struct AtParts;
 template <>
 struct AtParts<__bf16> {
-    static constexpr int kQ = 1, kH = 0, kP = 2;
+    static constexpr int kQ = 1, kP = 2;
 };
 template <>
 struct AtParts<float> {
-    static constexpr int kQ = 3, kH = 2, kP = 3;
+    static constexpr int kQ = 3, kP = 3;
 };
 
 __device__ __forceinline__ f4 mfma(b8 a, b8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-
-__device__ __forceinline__ f4 mfma(h8 a, h8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-
-// Eight values as N parts in half precision, the largest first.
-template <int N>
-__device__ __forceinline__ void parts(const float (&x)[8], h8 (&p)[N]) {
-#pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-        f2 r = {x[e], x[e + 1]};
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const h2 h = __builtin_convertvector(r, h2);
-            p[n][e] = h[0];
-            p[n][e + 1] = h[1];
-            r[0] = __builtin_fmaf((float)h[0], -1.0f, r[0]);
-            r[1] = __builtin_fmaf((float)h[1], -1.0f, r[1]);
-        }
-    }
-}
 
 // Eight values as N bf16 parts, the largest first.  What a part leaves is one
 // dot product: r - 1 * part + 0 * its neighbour, exact.  The pairs (-1, 0) and
@@ -133,12 +111,10 @@ __device__ __forceinline__ void parts(const float (&x)[8], b8 (&p)[N]) {
     }
 }
 
-// Two 4-bit values of byte J of w, times the power, as a pair of the type that
-// V8 is a vector of.
-template <int J, class V8>
+// Two 4-bit values of byte J of w, times the power.
+template <int J>
 __device__ __forceinline__ unsigned pair_of(unsigned w, float power) {
-    if constexpr (std::is_same<V8, h8>::value) return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, power, J));
-    else return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, J));
+    return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, J));
 }
 
 // A tile of 32 tokens of one head as a lane holds it.
@@ -192,7 +168,7 @@ __device__ __forceinline__ b8 key_frag(const AtKeys<DP>& t) {
     constexpr int kPerLane = KvLayout<DP>::kPowers / 2;    // powers of a half in a lane
     const unsigned w = t.w[A * (DP / 32) + KK];
     const float power = power_at<A * kPerLane + KK * kPerLane / (DP / 32)>(t.power);
-    u4 r = {pair_of<0, b8>(w, power), pair_of<1, b8>(w, power), pair_of<2, b8>(w, power), pair_of<3, b8>(w, power)};
+    u4 r = {pair_of<0>(w, power), pair_of<1>(w, power), pair_of<2>(w, power), pair_of<3>(w, power)};
     return __builtin_bit_cast(b8, r);
 }
 
@@ -210,34 +186,34 @@ __device__ __forceinline__ void add_scores(const AtKeys<DP>& x, const b8 (&q)[NT
 
 // Tiles 2 B and 2 B + 1 of the values as operands: rows are channels kRows i +
 // 2 B (+ 1), k the lane's eight tokens.
-template <int DP, int B, class V8>
-__device__ __forceinline__ void value_frags(const unsigned (&v)[DP / 16], const float (&power)[8], V8 (&f)[2]) {
+template <int DP, int B>
+__device__ __forceinline__ void value_frags(const unsigned (&v)[DP / 16], const float (&power)[8], b8 (&f)[2]) {
     u4 lo, hi;
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         unsigned x, y;
         if constexpr (DP == 64) {                 // a word holds two tokens
-            x = pair_of<B, V8>(v[p], power[2 * p]);
-            y = pair_of<B + 2, V8>(v[p], power[2 * p + 1]);
+            x = pair_of<B>(v[p], power[2 * p]);
+            y = pair_of<B + 2>(v[p], power[2 * p + 1]);
         } else if constexpr (DP == 128) {
-            x = pair_of<B, V8>(v[2 * p], power[2 * p]);
-            y = pair_of<B, V8>(v[2 * p + 1], power[2 * p + 1]);
+            x = pair_of<B>(v[2 * p], power[2 * p]);
+            y = pair_of<B>(v[2 * p + 1], power[2 * p + 1]);
         } else {                                  // two words a token
-            x = pair_of<B % 4, V8>(v[4 * p + B / 4], power[2 * p]);
-            y = pair_of<B % 4, V8>(v[4 * p + 2 + B / 4], power[2 * p + 1]);
+            x = pair_of<B % 4>(v[4 * p + B / 4], power[2 * p]);
+            y = pair_of<B % 4>(v[4 * p + 2 + B / 4], power[2 * p + 1]);
         }
         lo[p] = __builtin_amdgcn_perm(y, x, 0x05040100);
         hi[p] = __builtin_amdgcn_perm(y, x, 0x07060302);
     }
-    f[0] = __builtin_bit_cast(V8, lo);
-    f[1] = __builtin_bit_cast(V8, hi);
+    f[0] = __builtin_bit_cast(b8, lo);
+    f[1] = __builtin_bit_cast(b8, hi);
 }
 
-template <int DP, int NT, int NP, int B = 0, class V8>
-__device__ __forceinline__ void add_values(const unsigned (&v)[DP / 16], const float (&power)[8], const V8 (&p)[NT][NP],
+template <int DP, int NT, int NP, int B = 0>
+__device__ __forceinline__ void add_values(const unsigned (&v)[DP / 16], const float (&power)[8], const b8 (&p)[NT][NP],
                                            f4 (&o)[NT][DP / 16]) {
     if constexpr (B < DP / 32) {
-        V8 f[2];
+        b8 f[2];
         value_frags<DP, B>(v, power, f);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
@@ -258,10 +234,10 @@ __device__ __forceinline__ b8 bits(unsigned x) {
 }
 
 // The tile's probabilities into their sums and, times its values, the outputs.
-template <int DP, int NT, int N, class V8>
+template <int DP, int NT, int N>
 __device__ __forceinline__ void add_products(const unsigned (&v)[DP / 16], const float (&power)[8], const float (&w)[NT][8], f4 (&l)[NT],
                                              f4 (&o)[NT][DP / 16]) {
-    V8 p[NT][N], ones;
+    b8 p[NT][N], ones;
 #pragma unroll
     for (int e = 0; e < 8; ++e) ones[e] = 1.0f;
 #pragma unroll
@@ -322,7 +298,7 @@ __device__ __forceinline__ int by_length(const AttendArgs& a, int place, int ahe
 // tokens.
 template <int DP, class T, int NT, bool MASK>
 __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, NT>)) void k_attend(AttendArgs a) {
-    constexpr int NW = kAtWaves<DP, T, NT>, NQ = AtParts<T>::kQ, NP = AtParts<T>::kP, NH = AtParts<T>::kH, NK = DP / 32, ND = DP / 16;
+    constexpr int NW = kAtWaves<DP, T, NT>, NQ = AtParts<T>::kQ, NP = AtParts<T>::kP, NK = DP / 32, ND = DP / 16;
     using L = KvLayout<DP>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int rows = a.n * a.group, nrt = (rows + 16 * NT - 1) / (16 * NT);
@@ -401,15 +377,13 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     float sub[NT], raise[NT];
 
     // One pass over the wave's tiles; false where it has to be made again with
-    // care: where a value lies outside half precision's window (fp32 calls), or
-    // one that is not a number reached an output (bf16 calls; it may stand at a
-    // token that only other rows see, and 0 times it is not 0).  The careful
-    // pass takes values in bf16, and blocks that are not finite as zeros; a
-    // count of those that each row sees says which channels they spoil.
+    // care: where a value that is not a number reached an output (it may stand
+    // at a token that only other rows see, and 0 times it is not 0).  The
+    // careful pass takes blocks that are not finite as zeros, and is the same
+    // otherwise; a count of those that each row sees says which channels they
+    // spoil.
     auto pass = [&](auto careful) {
-        constexpr bool kCareful = decltype(careful)::value, kHalf = !kCareful && sizeof(T) == 4;
-        using V8 = typename std::conditional<kHalf, h8, b8>::type;
-        bool fits = true;
+        constexpr bool kCareful = decltype(careful)::value;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -454,7 +428,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
             // up, its values then, and the page of the one after it.  Past
             // the end it is the last tile again, so that the loads in flight
             // are the same on every path.
-            for (int tile = tile0; tile < t1 && fits; tile += NW) {
+            for (int tile = tile0; tile < t1; tile += NW) {
                 load_values(values, record, lane);
                 // the loads go out before the wait for the keys
                 __builtin_amdgcn_sched_barrier(0);
@@ -494,7 +468,6 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                     values.power[0] = (values.power[0] & (unsigned)in) | (0x7f7f7f7fu & ~(unsigned)in);
                     values.power[1] = (values.power[1] & (unsigned)(in >> 32)) | (0x7f7f7f7fu & ~(unsigned)(in >> 32));
                 }
-                if constexpr (kHalf) fits = !__any(((values.power[0] - kAtWindow) | (values.power[1] - kAtWindow)) & 0xe0e0e0e0u);
                 float power[8] = {power_at<0>(values.power[0]), power_at<1>(values.power[0]), power_at<2>(values.power[0]), power_at<3>(values.power[0]),
                                   power_at<0>(values.power[1]), power_at<1>(values.power[1]), power_at<2>(values.power[1]), power_at<3>(values.power[1])};
                 if constexpr (kCareful) {
@@ -532,13 +505,15 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
 #pragma unroll
                     for (int e = 0; e < 8; ++e) w[t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e / 4][e % 4], a.scale_log2, -sub[t]));
                 }
-                add_products<DP, NT, kHalf ? NH : NP, V8>(values.w, power, w, l, o);
+                add_products<DP, NT, NP>(values.w, power, w, l, o);
                 there = next_there;
                 missing |= !there;
             }
             if (missing && lane == 0) atomicOr(a.c.err, kErrKvPage);
         }
-        if constexpr (!kCareful && !kHalf) {
+        if constexpr (kCareful) {
+            return true;
+        } else {
             bool nan = false;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
@@ -546,9 +521,8 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                 for (int r = 0; r < ND; ++r)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) nan |= o[t][r][e] != o[t][r][e];
-            fits = !__any(nan);
+            return !__any(nan);
         }
-        return fits;
     };
     if (!pass(std::false_type())) pass(std::true_type());
 #pragma unroll

@@ -1,0 +1,57 @@
+"""Rows that the 4-bit cache's attention can get wrong.  u = 2^-24."""
+import numpy as np
+import pytest
+
+from paper_2607_19082_amd import wf
+from test_cache_gpu import DTYPE, U, filled, ints
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def device():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    wf.lib()  # fails loudly when the library is missing
+    torch.cuda.set_device(0)
+
+
+def attend(c, q, table, vis, dtype, **kw):
+    out = c.attend(q.to(DTYPE[dtype]).cuda(), table, ints(vis), **kw)
+    c.sync()
+    return out
+
+
+# ---- probabilities far below the largest ------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("dim,L,at", [(64, 288, 0), (64, 288, 150), (128, 288, 287), (256, 100, 3), (64, 9001, 0), (128, 9001, 9000),
+                                      (256, 9001, 4500), (128, 3, 1)])
+def test_small_probabilities_count(dim, L, at, dtype):
+    """One token holds nearly all of a row's weight and the value 0, so that the
+    outputs are the others' alone, d nats below it.
+
+    A score is one exact product, its power of two is off by 2 d u at most and
+    its probability by a few u more; sums as in the other tests: |out - ref| <=
+    A (4 (d + 4) + 2 (L + 64)) u, and bf16's 16 bits and rounding.  Each output
+    has one sign, so A = |ref|."""
+    g = np.random.default_rng(L + at)
+    far = (4, 8, 16, 20, 24, 40, 70)
+    k, v = torch.zeros((1, L, 1, dim)), torch.from_numpy(g.choice([0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], (1, L, 1, dim))).float()
+    k[0, :, 0, 0] = -1.0
+    k[0, at] = v[0, at] = 0.0
+    q = torch.zeros((1, len(far), 1, dim))
+    q[0, :, 0, 0] = torch.tensor(far, dtype=torch.float32)
+    c, table = filled(k, v)
+    out = attend(c, q, table, [[L] * len(far)], dtype, scale=1.0)[0, :, 0].float().cpu().numpy().astype(np.float64)
+    for i, d in enumerate(far):
+        p = np.exp(-float(d))
+        ref = p * v[0, :, 0].double().numpy().sum(0) / (1 + p * (L - 1))
+        tol = ref * (4 * (d + 4) + 2 * (L + 64)) * U
+        if dtype == "bf16":
+            tol = tol + ref * (2.0 ** -15 + 2.0 ** -8)
+        assert (np.abs(out[i] - ref) <= tol).all(), (d, float((np.abs(out[i] - ref) / ref).max()))
+    c.close()
