@@ -491,16 +491,16 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                     for (int e = 1; e < 8; ++e) top = __builtin_elementwise_maximum(top, s[t][e / 4][e % 4]);
                     top *= a.scale_log2;
                     if (__any(top > raise[t])) {
+                        // only the rows that pass their own: what another row
+                        // sees does not change this one's bits
                         top = lane_rows(top, [](float x, float y) { return fmaxf(x, y); });
-                        const bool none = raise[t] == -INFINITY;
-                        const float most = none ? top : fmaxf(sub[t] + kAtLift, top), by = none ? 0.0f : exp2f(sub[t] + kAtLift - most);
-                        if (most != -INFINITY) {
-                            sub[t] = most - kAtLift;
-                            raise[t] = most + kAtSlack;
+                        const bool none = raise[t] == -INFINITY, up = top > raise[t];
+                        const float to = up ? top - kAtLift : sub[t], by = none ? 0.0f : exp2f(sub[t] - to);
+                        sub[t] = to;
+                        raise[t] = up ? top + kAtSlack : raise[t];
 #pragma unroll
-                            for (int r = 0; r < ND; ++r) o[t][r] *= by;
-                            l[t] *= by;
-                        }
+                        for (int r = 0; r < ND; ++r) o[t][r] *= by;
+                        l[t] *= by;
                     }
 #pragma unroll
                     for (int e = 0; e < 8; ++e) w[t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e / 4][e % 4], a.scale_log2, -sub[t]));

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 from paper_2607_19082_amd import wf
-from test_cache_gpu import DTYPE, U, filled, ints
+from test_cache_gpu import DTYPE, U, draw, filled, ints
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +55,55 @@ def test_small_probabilities_count(dim, L, at, dtype):
             tol = tol + ref * (2.0 ** -15 + 2.0 ** -8)
         assert (np.abs(out[i] - ref) <= tol).all(), (d, float((np.abs(out[i] - ref) / ref).max()))
     c.close()
+
+
+# ---- what other rows see -------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("dim,L,group", [(64, 200, 2), (128, 3000, 4), (256, 500, 1), (128, 70, 8)])
+def test_bits_do_not_depend_on_what_a_row_does_not_see(dim, L, group, dtype):
+    """A row's bits stay, whatever lies at tokens that its mask or its prefix
+    leaves out, where other rows of the call see them too: ordinary values,
+    large keys, large or tiny values, blocks that are not finite, tokens never
+    written (those that no row sees)."""
+    g = np.random.default_rng(17)
+    n = 5
+    k, v = draw((1, L, 1, dim), dtype, 1), draw((1, L, 1, dim), dtype, 2)
+    q = draw((1, n, group, dim), dtype, 3, 0.0)
+    hidden = g.random(L) < 0.3
+    hidden[0] = False
+    hidden[L - 20:] = True
+    # rows 0 to 2 never see the hidden tokens; rows 3 and 4 see those of them in `shown`
+    for shown in (np.zeros(L, bool), hidden & (np.arange(L) < L - 20)):
+        m = np.tile(~hidden, (1, n, 1))
+        m[0, 3:] |= shown
+        m[0, 1] &= g.random(L) < 0.5
+        vis = [[L - 20, L - 20, L // 2, L - 20, L - 20]]
+        first = None
+        for what in ("as drawn", "large keys", "large values", "tiny values", "nan", "inf", "never written"):
+            kw, vw = k.clone(), v.clone()
+            h = torch.from_numpy(hidden)
+            if what == "large keys":
+                kw[:, h] *= 64
+            elif what == "large values":
+                vw[:, h] *= 2.0 ** 60
+            elif what == "tiny values":
+                vw[:, h] *= 2.0 ** -60
+            elif what == "nan":
+                kw[:, h], vw[:, h] = float("nan"), float("nan")
+            elif what == "inf":
+                vw[:, h, :, ::40] = float("inf")
+            c, table = filled(kw, vw)
+            if what == "never written":
+                if shown.any():
+                    c.close()
+                    continue
+                c.close()
+                c = wf.Cache(1, dim, c.pages)
+                for t in np.flatnonzero(~hidden):
+                    c.write(k[:, t:t + 1].cuda(), v[:, t:t + 1].cuda(), table, ints([t]))
+            out = attend(c, q, table, vis, dtype, mask=torch.from_numpy(m).cuda())[:, :3]
+            first = out if first is None else first
+            assert torch.equal(out, first), (what, bool(shown.any()))
+            c.close()
