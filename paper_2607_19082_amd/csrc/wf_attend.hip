@@ -71,6 +71,11 @@ constexpr float kAtSlack = 8.0f;
 // first) is a normal number down to 2^-109 of the row's largest; the sums that
 // divide them are too.
 constexpr float kAtLift = 7.0f;
+// Rows whose maximum lies beyond this (in powers of two) round the product of
+// score and scale before they subtract the maximum.  Below, one multiply-add
+// takes the exact product, which passes its rounded value, the maximum, by half
+// a unit in the last place: 1/4 here, but 32 and more from 2^29 on.
+constexpr float kAtFar = 4194304.0f;
 
 // bf16 parts of queries and of probabilities
 template <class T>
@@ -249,7 +254,13 @@ __device__ __forceinline__ void add_products(const unsigned (&v)[DP / 16], const
     add_values<DP, NT, N>(v, power, p, o);
 }
 
-// Weight of a partial result with maximum m and sum l; 0 where it saw no token.
+// x y - z with the product rounded by itself
+__device__ __forceinline__ float product_less(float x, float y, float z) {
+#pragma clang fp contract(off)
+    return x * y - z;
+}
+
+// Weight of a partial result with maximum m (less the lift) and sum l; 0 where it saw no token.
 __device__ __forceinline__ float at_weight(float m, float l, float most) {
     const float w = __builtin_amdgcn_exp2f(m - most);
     return m == -INFINITY && l == 0.0f ? 0.0f : (m == most ? 1.0f : w);
@@ -375,6 +386,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     // the row's maximum so far, and the score that raises it (none: 0 and
     // -infinity)
     float sub[NT], raise[NT];
+    bool far[NT];                          // of any row of the wave
 
     // One pass over the wave's tiles; false where it has to be made again with
     // care: where a value that is not a number reached an output (it may stand
@@ -391,6 +403,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
             l[t] = bad[t] = f4{0, 0, 0, 0};
             raise[t] = -INFINITY;
             sub[t] = 0.0f;
+            far[t] = false;
         }
         const int tile0 = t0 + wave;
         if (tile0 < t1) {
@@ -498,12 +511,19 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                         const float to = up ? top - kAtLift : sub[t], by = none ? 0.0f : exp2f(sub[t] - to);
                         sub[t] = to;
                         raise[t] = up ? top + kAtSlack : raise[t];
+                        far[t] = __any(fabsf(to) >= kAtFar);
 #pragma unroll
                         for (int r = 0; r < ND; ++r) o[t][r] *= by;
                         l[t] *= by;
                     }
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) w[t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e / 4][e % 4], a.scale_log2, -sub[t]));
+                    for (int e = 0; e < 8; ++e) w[t][e] = __builtin_fmaf(s[t][e / 4][e % 4], a.scale_log2, -sub[t]);
+                    if (far[t])
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (fabsf(sub[t]) >= kAtFar) w[t][e] = product_less(s[t][e / 4][e % 4], a.scale_log2, sub[t]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) w[t][e] = __builtin_amdgcn_exp2f(w[t][e]);
                 }
                 add_products<DP, NT, NP>(values.w, power, w, l, o);
                 there = next_there;
@@ -543,7 +563,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     for (int t = 0; t < NT; ++t) {
         if (t) __syncthreads();
         if (lane < 16) {
-            sm[wave][lane] = raise[t] == -INFINITY ? -INFINITY : sub[t] + kAtLift;
+            sm[wave][lane] = raise[t] == -INFINITY ? -INFINITY : sub[t];
             sl[wave][lane] = l[t][0];
         }
 #pragma unroll

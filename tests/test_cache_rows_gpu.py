@@ -2,6 +2,7 @@
 import numpy as np
 import pytest
 
+from oracle import cache as oracle
 from paper_2607_19082_amd import wf
 from test_cache_gpu import DTYPE, U, draw, filled, ints
 
@@ -107,3 +108,37 @@ def test_bits_do_not_depend_on_what_a_row_does_not_see(dim, L, group, dtype):
             first = out if first is None else first
             assert torch.equal(out, first), (what, bool(shown.any()))
             c.close()
+
+
+# ---- large scores -----------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("dim,L", [(64, 90), (128, 700), (256, 300), (64, 9001), (128, 9001)])
+def test_large_scores(dim, L, dtype):
+    """Finite scores from 2^20 to 2^100 with gaps of thousands between unequal
+    ones: a row is the mean of the values at its largest score, which are held
+    by several tokens of several waves and splits."""
+    g = np.random.default_rng(L + dim)
+    k, v = torch.zeros((1, L, 1, dim)), draw((1, L, 1, dim), dtype, 2).float()
+    x = g.integers(-4, 5, L)
+    x[g.random(L) < 0.02] = 6
+    x[g.random(L) < 0.02] = -6
+    x[[1, L - 1]], x[[0, L - 2]] = 6, -6
+    k[0, :, 0, 0] = torch.from_numpy(x).float()
+    powers = np.concatenate([np.arange(20, 36), [40, 60, 100]])
+    q = torch.zeros((1, 2 * len(powers), 1, dim))
+    q[0, :, 0, 0] = torch.from_numpy(np.ldexp(g.uniform(1, 2, 2 * len(powers)), np.repeat(powers, 2)) * np.tile([1, -1], len(powers)))
+    q = q.to(DTYPE[dtype])
+    c, table = filled(k.to(DTYPE[dtype]), v.to(DTYPE[dtype]))
+    vq = oracle.quantise(v.to(DTYPE[dtype]).float().numpy())[0, :, 0]
+    for scale in (1.0, 0.125, 0.1):
+        out = attend(c, q, table, [[L] * q.shape[1]], dtype, scale=scale)[0, :, 0].float().cpu().numpy().astype(np.float64)
+        for i in range(q.shape[1]):
+            top = x == (6 if i % 2 == 0 else -6)
+            ref, mag = vq[top].mean(0), np.abs(vq[top]).mean(0)
+            tol = mag * 2 * (L + 64) * U
+            if dtype == "bf16":
+                tol = tol + mag * 2.0 ** -15 + np.abs(ref) * 2.0 ** -8
+            assert (np.abs(out[i] - ref) <= tol).all(), (scale, i, powers[i // 2], out[i][:4], ref[:4])
+    c.close()
