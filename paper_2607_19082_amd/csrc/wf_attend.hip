@@ -260,10 +260,17 @@ __device__ __forceinline__ float product_less(float x, float y, float z) {
     return x * y - z;
 }
 
-// Weight of a partial result with maximum m (less the lift) and sum l; 0 where it saw no token.
+// Weight of a partial result with maximum m (less the lift) and sum l; 0 where
+// it saw no token.  Where the tokens it saw are all at -infinity, l is 1 and o
+// 0: nothing beside a finite maximum, and 0 / 0 where the row has none.
 __device__ __forceinline__ float at_weight(float m, float l, float most) {
     const float w = __builtin_amdgcn_exp2f(m - most);
     return m == -INFINITY && l == 0.0f ? 0.0f : (m == most ? 1.0f : w);
+}
+
+// What a row's joined sum divides it by.
+__device__ __forceinline__ float at_scale(float most, float sum) {
+    return sum == 0.0f ? 0.0f : (most == -INFINITY ? __builtin_nanf("") : 1.0f / sum);
 }
 
 // Eight channels of a row, into the output.
@@ -387,6 +394,8 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     // -infinity)
     float sub[NT], raise[NT];
     bool far[NT];                          // of any row of the wave
+    unsigned seen[NT];                     // not 0: the row sees a token of the lane's
+    bool all;                              // every row sees a whole tile
 
     // One pass over the wave's tiles; false where it has to be made again with
     // care: where a value that is not a number reached an output (it may stand
@@ -396,6 +405,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     // spoil.
     auto pass = [&](auto careful) {
         constexpr bool kCareful = decltype(careful)::value;
+        all = false;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -404,6 +414,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
             raise[t] = -INFINITY;
             sub[t] = 0.0f;
             far[t] = false;
+            seen[t] = 0;
         }
         const int tile0 = t0 + wave;
         if (tile0 < t1) {
@@ -471,9 +482,11 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                             sees[t] |= (unsigned)on << e;
                             s[t][e / 4][e % 4] = on ? s[t][e / 4][e % 4] : -INFINITY;
                         }
+                        seen[t] |= sees[t];
                     }
                 }
                 if constexpr (MASK) load_mask(tile + NW);
+                all |= !edge;
                 if (edge) {
                     // past the last token that any row sees, a page holds anything
                     const int n = max(0, min(8, there ? most - at : 0));
@@ -562,9 +575,11 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         if (t) __syncthreads();
+        const float some = lane_rows(all || seen[t] ? 1.0f : 0.0f, [](float x, float y) { return fmaxf(x, y); });
         if (lane < 16) {
-            sm[wave][lane] = raise[t] == -INFINITY ? -INFINITY : sub[t];
-            sl[wave][lane] = l[t][0];
+            const bool none = raise[t] == -INFINITY;
+            sm[wave][lane] = none ? -INFINITY : sub[t];
+            sl[wave][lane] = none ? l[t][0] + some : l[t][0];
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -585,7 +600,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                 by[w] = at_weight(sm[w][c], sl[w][c], most);
                 sum += by[w] * sl[w][c];
             }
-            const float scale = a.splits > 1 ? 1.0f : (sum == 0.0f ? 0.0f : 1.0f / sum);
+            const float scale = a.splits > 1 ? 1.0f : at_scale(most, sum);
 #pragma unroll
             for (int w = 0; w < NW; ++w) sm[w][c] = by[w] * scale;
             top[c] = most;
@@ -652,7 +667,7 @@ __global__ __launch_bounds__(kAtJoin) void k_attend_join(AttendArgs a) {
             sum += z[k][0] * z[k][1];
         }
         sum = lanes64(sum, [](float x, float y) { return x + y; });
-        const float scale = sum == 0.0f ? 0.0f : 1.0f / sum;
+        const float scale = at_scale(most, sum);
 #pragma unroll
         for (int k = 0; k < K; ++k) weight[k * 64 + lane] = z[k][0] * scale;
     }

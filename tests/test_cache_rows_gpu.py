@@ -142,3 +142,38 @@ def test_large_scores(dim, L, dtype):
                 tol = tol + mag * 2.0 ** -15 + np.abs(ref) * 2.0 ** -8
             assert (np.abs(out[i] - ref) <= tol).all(), (scale, i, powers[i // 2], out[i][:4], ref[:4])
     c.close()
+
+
+# ---- scores that are infinite ---------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("dim,L", [(64, 40), (128, 700), (256, 300), (64, 9001)])
+def test_scores_of_minus_infinity(dim, L, dtype):
+    """Rows that see tokens, all at -infinity, are NaN (0 / 0); tokens at
+    -infinity beside finite ones have no part; rows that see nothing are zeros."""
+    k, v = torch.zeros((1, L, 1, dim)), draw((1, L, 1, dim), dtype, 2)
+    k[0, :, 0, 0] = -6.0
+    k[0, L // 2:, 0, 1] = -4.0
+    q = torch.zeros((1, 6, 1, dim))
+    q[0, 0, 0, :2] = torch.tensor([float("inf"), 1.0])     # -infinity throughout
+    q[0, 1, 0, :2] = torch.tensor([float("inf"), 1.0])     # one token of it
+    q[0, 2, 0, 1] = 3e38                                   # finite products below the range in the later half
+    q[0, 3] = q[0, 2]                                      # and no other tokens seen
+    q[0, 4, 0, 0] = float("inf")                           # sees nothing
+    q[0, 5, 0, 0] = 1.0
+    c, table = filled(k.to(DTYPE[dtype]), v)
+    m = np.ones((1, 6, L), bool)
+    m[0, 1, np.arange(L) != L // 3] = False
+    m[0, 3, :L // 2] = False
+    m[0, 4] = False
+    out = attend(c, q, table, [[L] * 6], dtype, mask=torch.from_numpy(m).cuda(), scale=1.0)[0, :, 0].float().cpu().numpy()
+    nothing = attend(c, q, table, [[0] * 5 + [L]], dtype, max_visible=L)[0, :, 0].float().cpu().numpy()
+    vq = oracle.quantise(v.float().numpy())[0, :, 0]
+    for i, see in ((2, slice(0, L // 2)), (5, slice(0, L))):
+        ref, mag = vq[see].mean(0), np.abs(vq[see]).mean(0)
+        tol = mag * 2 * (L + 64) * U + (mag * 2.0 ** -15 + np.abs(ref) * 2.0 ** -8 if dtype == "bf16" else 0)
+        assert (np.abs(out[i] - ref) <= tol).all(), i
+    assert np.isnan(out[[0, 1, 3]]).all() and (out[4] == 0).all()
+    assert (nothing[:5] == 0).all() and np.isfinite(nothing[5]).all()
+    c.close()
