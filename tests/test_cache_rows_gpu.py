@@ -2,6 +2,7 @@
 import numpy as np
 import pytest
 
+import cache_precision as cp
 from oracle import cache as oracle
 from paper_2607_19082_amd import wf
 from test_cache_gpu import DTYPE, U, draw, filled, ints
@@ -176,4 +177,21 @@ def test_scores_of_minus_infinity(dim, L, dtype):
         assert (np.abs(out[i] - ref) <= tol).all(), i
     assert np.isnan(out[[0, 1, 3]]).all() and (out[4] == 0).all()
     assert (nothing[:5] == 0).all() and np.isfinite(nothing[5]).all()
+    c.close()
+
+
+# ---- the bits of a probability ----------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("dim,L,sees", cp.CASES)
+def test_bits_of_a_probability(dim, L, sees, dtype):
+    """24 bits in fp32 calls and 16 in bf16 ones, by bars that fewer do not
+    pass (derived in cache_precision.py, and shown on a model on the CPU)."""
+    q, k, v, mask = cp.case(dtype, dim, L, sees)
+    ref, mag, _ = oracle.attend(q, k, v, [L] * len(q), mask, 1.0)
+    c, table = filled(*(torch.from_numpy(x)[None].to(DTYPE[dtype]) for x in (k, v)))
+    out = attend(c, torch.from_numpy(q)[None], table, [[L] * len(q)], dtype, mask=torch.from_numpy(mask)[None].cuda(), scale=1.0)
+    got, bar = cp.misses(dtype, out[0].float().cpu().numpy(), ref, mag)
+    assert got <= bar, (got / U, bar / U)
     c.close()
