@@ -516,7 +516,9 @@ typedef struct {
 
 /* Build a cache: the pool (zeros: a token that was never written reads as 0)
  * and the workspace of its attention calls (64 Ki rows of dim + 2 floats).
- * Synchronous; uses the current HIP device, on which all its calls run.
+ * Synchronous; uses the current HIP device, on which all its calls run, whatever
+ * device is current for them (a stream of theirs is that device's; NULL: its
+ * default stream).
  * Errors: WF_E_INVALID, WF_E_UNSUPPORTED, WF_E_NOMEM, WF_E_HIP. */
 int wf_cache_plan(const wf_cache_desc *desc, wf_cache_t *out);
 

@@ -252,11 +252,37 @@ void launch_kv_read(const KvCache& c, int precision, const KvRows& k, const KvRo
 
 struct Cache {
     KvCache c{};
+    int device = 0;                  // its memory's, on which its kernels run
     void* memory = nullptr;          // one allocation: the error word, the pool, the workspace
     float* work = nullptr;           // partial results of split attention calls
 };
 
 static int kv_fail(hipError_t e, const char* what) { return fail(WF_E_HIP, std::string(what) + ": " + hipGetErrorString(e)); }
+
+// Makes a cache's device current for a call.  A default stream is that of the
+// current device, and a host thread may have another one current (a new thread
+// begins with device 0).
+class OnDevice {
+public:
+    explicit OnDevice(int device) {
+        e_ = hipGetDevice(&was_);
+        if (e_ == hipSuccess && was_ != device) {
+            e_ = hipSetDevice(device);
+            changed_ = e_ == hipSuccess;
+        }
+    }
+    ~OnDevice() {
+        if (changed_) (void)hipSetDevice(was_);
+    }
+    OnDevice(const OnDevice&) = delete;
+    OnDevice& operator=(const OnDevice&) = delete;
+    hipError_t error() const { return e_; }
+
+private:
+    int was_ = 0;
+    bool changed_ = false;
+    hipError_t e_;
+};
 
 static void free_cache(Cache* c) {
     if (!c) return;
@@ -318,7 +344,12 @@ int wf_cache_plan(const wf_cache_desc* d, wf_cache_t* out) try {
     // (a record is a multiple of 64 bytes)
     const size_t head = 256, pool = (k.page_bytes() * k.pages + 255) / 256 * 256;
     const size_t work = (size_t)kAttendWorkRows * (k.dp + 2) * sizeof(float);
-    hipError_t e = hipMalloc(&c->memory, head + pool + work);
+    hipError_t e = hipGetDevice(&c->device);
+    if (e != hipSuccess) {
+        free_cache(c);
+        return kv_fail(e, "hipGetDevice");
+    }
+    e = hipMalloc(&c->memory, head + pool + work);
     if (e != hipSuccess) {
         (void)hipGetLastError();     // reported here, not by the next launch
         c->memory = nullptr;
@@ -351,6 +382,8 @@ int wf_cache_write(wf_cache_t cache, int32_t precision, const wf_rows* k, const 
     int rc = kv_tokens(c, precision, B, n, table, table_pages, first, counts, &a);
     if (rc != WF_OK || !B || !n) return rc;
     if ((rc = kv_rows(k, precision, "k", &kr)) != WF_OK || (rc = kv_rows(v, precision, "v", &vr)) != WF_OK) return rc;
+    const OnDevice on(c->device);
+    if (on.error() != hipSuccess) return kv_fail(on.error(), "the cache's device");
     launch_kv_write(c->c, precision, kr, vr, a, stream);
     return kv_launched("wf_cache_write");
 } catch (...) {
@@ -365,6 +398,8 @@ int wf_cache_read(wf_cache_t cache, int32_t precision, const wf_rows* k, const w
     int rc = kv_tokens(c, precision, B, n, table, table_pages, first, counts, &a);
     if (rc != WF_OK || !B || !n) return rc;
     if ((rc = kv_rows(k, precision, "k", &kr)) != WF_OK || (rc = kv_rows(v, precision, "v", &vr)) != WF_OK) return rc;
+    const OnDevice on(c->device);
+    if (on.error() != hipSuccess) return kv_fail(on.error(), "the cache's device");
     launch_kv_read(c->c, precision, kr, vr, a, stream);
     return kv_launched("wf_cache_read");
 } catch (...) {
@@ -399,6 +434,8 @@ int wf_cache_attend(wf_cache_t cache, int32_t precision, const wf_rows* q, const
     if (attend_plan(a, precision) >= 1LL << 32) return fail(WF_E_UNSUPPORTED, "2^32 or more threads in one call");
     a.part_o = c->work;
     a.part_ml = c->work + (size_t)kAttendWorkRows * c->c.dp;
+    const OnDevice on(c->device);
+    if (on.error() != hipSuccess) return kv_fail(on.error(), "the cache's device");
     launch_attend(a, precision, stream);
     return kv_launched("wf_cache_attend");
 } catch (...) {
@@ -408,6 +445,8 @@ int wf_cache_attend(wf_cache_t cache, int32_t precision, const wf_rows* q, const
 int wf_cache_sync(wf_cache_t cache, hipStream_t stream) try {
     Cache* c = reinterpret_cast<Cache*>(cache);
     if (!c) return fail(WF_E_INVALID, "cache is NULL");
+    const OnDevice on(c->device);
+    if (on.error() != hipSuccess) return kv_fail(on.error(), "the cache's device");
     int err = 0;
     hipError_t e = hipStreamSynchronize(stream);
     if (e == hipSuccess) e = hipMemcpy(&err, c->c.err, sizeof err, hipMemcpyDeviceToHost);

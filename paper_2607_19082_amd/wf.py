@@ -465,9 +465,9 @@ class Cache:
     Token t of sequence b lies in page table[b, t // page].  Tensors are torch
     tensors on the HIP device that was current at the plan, fp32 or bf16 where they hold channels
     (contiguous; sequence, token and head may have any strides) and contiguous
-    int32 elsewhere.  Calls are asynchronous on the given (default: current)
-    torch stream; one attend call in flight per cache.  sync() waits and raises
-    what a kernel found wrong."""
+    int32 elsewhere.  Calls are asynchronous on the given (default: that device's
+    current) torch stream, whatever device is current; one attend call in flight
+    per cache.  sync() waits and raises what a kernel found wrong."""
 
     def __init__(self, heads, dim, pages, page=64):
         import torch
@@ -610,4 +610,4 @@ class Cache:
         return out
 
     def sync(self, stream=None):
-        _check(lib().wf_cache_sync(self._h, _stream_handle(stream)))
+        _check(self._lib.wf_cache_sync(self._h, self._stream(stream)))

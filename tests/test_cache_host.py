@@ -1,0 +1,97 @@
+"""The 4-bit cache's host code on stand-ins for the HIP calls (no GPU needed):
+which device and stream its calls use.  Each test runs in a process of its own,
+where the stand-ins (hip_stub.cpp) are loaded before the library."""
+import os
+import subprocess
+import sys
+
+import pytest
+
+from paper_2607_19082_amd import wf
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+START = r'''
+import ctypes, sys
+sys.path.insert(0, ROOT)
+stub = ctypes.CDLL(STUB, mode=ctypes.RTLD_GLOBAL)
+from paper_2607_19082_amd import wf
+L = wf.lib()
+MALLOC, FREE, MEMSET, MEMCPY, MEMCPY_ASYNC, SYNC, LAUNCH, DEVICE_SYNC = range(1, 9)
+class Call(ctypes.Structure):
+    _fields_ = [("what", ctypes.c_int), ("device", ctypes.c_int), ("stream", ctypes.c_void_p), ("bytes", ctypes.c_uint64),
+                ("grid", ctypes.c_uint32), ("block", ctypes.c_uint32)]
+num = lambda name: ctypes.c_int.in_dll(stub, name)
+def calls(f=None, *args):
+    """What a call does: (its return value, the HIP calls)."""
+    num("stub_n").value = 0
+    rc = f(*args) if f else None
+    return rc, list((Call * 4096).in_dll(stub, "stub_calls")[:num("stub_n").value])
+def plan(*desc):
+    h = ctypes.c_void_p()
+    rc, made = calls(L.wf_cache_plan, ctypes.byref(wf.CacheDesc(*desc)), ctypes.byref(h))
+    assert rc == 0, L.wf_last_error()
+    return h, sum(c.bytes for c in made if c.what == MALLOC)
+rows = wf.Rows(0x1000, 1 << 20, 1 << 12, 1 << 8)
+P = 0x2000                                          # a device address, never followed
+def write(h, B, n, stream=None, pages=64):
+    return calls(L.wf_cache_write, h, 1, rows, rows, B, n, P, pages, P, None, stream)
+def read(h, B, n, stream=None, pages=64):
+    return calls(L.wf_cache_read, h, 1, rows, rows, B, n, P, pages, P, None, stream)
+def attend(h, B, n, hq, most, stream=None, precision=1, pages=1 << 15):
+    return calls(L.wf_cache_attend, h, precision, rows, rows, B, n, hq, P, pages, P, None, None, most, 1.0, stream)
+'''
+
+
+@pytest.fixture(scope="module")
+def run(tmp_path_factory):
+    if not os.path.exists(wf.LIB_PATH):
+        from paper_2607_19082_amd import build
+        build.build()
+    d = tmp_path_factory.mktemp("stub")
+    stub = str(d / "libstub.so")
+    subprocess.run(["g++", "-O1", "-shared", "-fPIC", os.path.join(ROOT, "tests", "hip_stub.cpp"), "-o", stub], check=True)
+
+    def go(code):
+        head = f"ROOT, STUB = {ROOT!r}, {stub!r}\n"
+        r = subprocess.run([sys.executable, "-c", head + START + code + "\nprint('done')"], capture_output=True, text=True, timeout=120)
+        assert r.returncode == 0 and r.stdout.endswith("done\n"), r.stdout + r.stderr
+
+    return go
+
+
+def test_calls_run_on_the_caches_device(run):
+    """A cache of device 1 used while device 0 is current: its launches, and
+    what sync does, find device 1 current, and device 0 is current again after."""
+    run(r'''
+num("stub_device").value = 1
+h, _ = plan(8, 128, 64, 64)
+num("stub_device").value = 0
+for f, args in ((write, (h, 2, 3)), (read, (h, 2, 3)), (attend, (h, 1, 1, 32, 1000)), (attend, (h, 1, 1, 32, 100000))):
+    for stream in (None, 0x77):
+        rc, made = f(*args, stream=stream)
+        assert rc == 0 and made and all(c.what == LAUNCH and c.device == 1 and c.stream == stream for c in made), f
+        assert num("stub_device").value == 0
+rc, made = calls(L.wf_cache_sync, h, 0x77)
+assert rc == 0 and made and all(c.device == 1 for c in made)
+assert num("stub_device").value == 0
+''')
+
+
+def test_the_bindings_sync_waits_for_the_caches_device():
+    """Cache.sync without a stream waits for the current stream of the cache's
+    device, as the calls use it."""
+    class Lib:
+        def wf_cache_sync(self, handle, stream):
+            self.got = getattr(stream, "value", stream)
+            return 0
+
+    class Stream:
+        cuda_stream = 55
+
+    c = wf.Cache.__new__(wf.Cache)
+    c._h, c._device, c._lib, c._current = None, 3, Lib(), lambda device: 1000 + device
+    c.sync()
+    assert c._lib.got == 1003
+    c.sync(Stream)
+    assert c._lib.got == 55
