@@ -579,7 +579,8 @@ int wf_cache_attend(wf_cache_t cache, int32_t precision, const wf_rows *q, const
                     hipStream_t stream);
 
 /* Wait for `stream` and report an error that the cache's kernels recorded
- * (see the calls above).  Clears it. */
+ * (see the calls above), on this stream or another.  Clears it; what is
+ * recorded while it does so is reported then or by the next one. */
 int wf_cache_sync(wf_cache_t cache, hipStream_t stream);
 
 /* Release a cache.  NULL is ignored. */

@@ -1,5 +1,6 @@
 // The 4-bit key/value cache: its plan, and the kernels that quantise tokens
 // into its pages and read them back.  Layout and format: wf_cache.h.
+#include <atomic>
 #include <cmath>
 #include <new>
 
@@ -248,12 +249,21 @@ void launch_kv_read(const KvCache& c, int precision, const KvRows& k, const KvRo
     else launch_kv_dp<float>(false, c, k, v, a, st);
 }
 
+// Takes the error word: what kernels on other streams record meanwhile is
+// either taken or stays for the next time.
+__global__ void k_kv_take_errors(int* err, int* out) { *out = atomicExch(err, 0); }
+
 // ---- plan and entry points ------------------------------------------------------
+
+constexpr unsigned kKvHead = 256, kKvTaken = kKvHead / sizeof(int) - 1;   // (that many syncs may be under way together)
 
 struct Cache {
     KvCache c{};
     int device = 0;                  // its memory's, on which its kernels run
-    void* memory = nullptr;          // one allocation: the error word, the pool, the workspace
+    // one allocation: the error word and kKvTaken words that syncs take it to, the
+    // pool, the workspace
+    void* memory = nullptr;
+    std::atomic<unsigned> syncs{0};
     float* work = nullptr;           // partial results of split attention calls
 };
 
@@ -342,7 +352,7 @@ int wf_cache_plan(const wf_cache_desc* d, wf_cache_t* out) try {
     k.dp = d->dim <= 64 ? 64 : (d->dim <= 128 ? 128 : 256);
     while ((1 << k.page_shift) < d->page) ++k.page_shift;
     // (a record is a multiple of 64 bytes)
-    const size_t head = 256, pool = (k.page_bytes() * k.pages + 255) / 256 * 256;
+    const size_t head = kKvHead, pool = (k.page_bytes() * k.pages + 255) / 256 * 256;
     const size_t work = (size_t)kAttendWorkRows * (k.dp + 2) * sizeof(float);
     hipError_t e = hipGetDevice(&c->device);
     if (e != hipSuccess) {
@@ -447,10 +457,14 @@ int wf_cache_sync(wf_cache_t cache, hipStream_t stream) try {
     if (!c) return fail(WF_E_INVALID, "cache is NULL");
     const OnDevice on(c->device);
     if (on.error() != hipSuccess) return kv_fail(on.error(), "the cache's device");
-    int err = 0;
+    int err = 0, *taken = c->c.err + 1 + c->syncs++ % kKvTaken;
     hipError_t e = hipStreamSynchronize(stream);
-    if (e == hipSuccess) e = hipMemcpy(&err, c->c.err, sizeof err, hipMemcpyDeviceToHost);
-    if (e == hipSuccess && err) e = hipMemset(c->c.err, 0, sizeof err);
+    if (e == hipSuccess) {
+        hipLaunchKernelGGL(k_kv_take_errors, dim3(1), dim3(1), 0, stream, c->c.err, taken);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess) e = hipMemcpyAsync(&err, taken, sizeof err, hipMemcpyDeviceToHost, stream);
+    if (e == hipSuccess) e = hipStreamSynchronize(stream);
     if (e != hipSuccess) return kv_fail(e, "wf_cache_sync");
     if (err & kErrKvPage) return fail(WF_E_INVALID, "a page table entry lies outside the pool");
     if (err & kErrKvRange) return fail(WF_E_CAPACITY, "a token lies past its page table, or a row sees more than max_visible tokens");

@@ -1,6 +1,7 @@
 """The 4-bit cache's host code on stand-ins for the HIP calls (no GPU needed):
-which device and stream its calls use.  Each test runs in a process of its own,
-where the stand-ins (hip_stub.cpp) are loaded before the library."""
+which device and stream its calls use, and what sync reports.  Each test runs in
+a process of its own, where the stand-ins (hip_stub.cpp) are loaded before the
+library."""
 import os
 import subprocess
 import sys
@@ -75,6 +76,22 @@ for f, args in ((write, (h, 2, 3)), (read, (h, 2, 3)), (attend, (h, 1, 1, 32, 10
 rc, made = calls(L.wf_cache_sync, h, 0x77)
 assert rc == 0 and made and all(c.device == 1 for c in made)
 assert num("stub_device").value == 0
+''')
+
+
+def test_sync_loses_no_error(run):
+    """An error that a kernel on another stream records as soon as sync has
+    copied the word is reported by the next sync; all of it goes by the stream
+    that sync is given."""
+    run(r'''
+h, _ = plan(2, 64, 4, 64)
+sync = lambda: calls(L.wf_cache_sync, h, 0x77)
+num("stub_word").value, num("stub_late").value = 1, 2
+rc, made = sync()
+assert rc == wf.WF_E_CAPACITY and sync()[0] == wf.WF_E_INVALID and sync()[0] == 0
+num("stub_word").value, num("stub_late").value = 0, 1
+assert sync()[0] == 0 and sync()[0] == wf.WF_E_CAPACITY and sync()[0] == 0
+assert made and all(c.stream == 0x77 for c in made) and made[-1].what == SYNC
 ''')
 
 
