@@ -560,8 +560,9 @@ int wf_cache_read(wf_cache_t cache, int32_t precision, const wf_rows *k, const w
  *                causal chunk, 0 for a row that is not in use)
  *   mask         NULL, or DEVICE bytes: mask[b * mask_stride[0] + i *
  *                mask_stride[1] + j], j < max_visible (mask_stride is HOST)
- *   max_visible  no row sees more (it sizes the launch); a row that does is
- *                cut there, and the next wf_cache_sync returns WF_E_CAPACITY
+ *   max_visible  no row sees more (it sizes the launch; at most 2^31 - 65); a
+ *                row that does is cut there, and the next wf_cache_sync returns
+ *                WF_E_CAPACITY
  *   scale        positive; 1 / sqrt(dim) as a rule
  * Tokens in a page outside the pool are left out, and the next wf_cache_sync
  * returns WF_E_INVALID.  Sums are held in fp32, before they are divided (they
@@ -571,7 +572,7 @@ int wf_cache_read(wf_cache_t cache, int32_t precision, const wf_rows *k, const w
  * whatever lies at tokens that a row does not see.  Asynchronous on `stream`;
  * one call in flight per cache (the workspace is shared by its calls).
  * Errors: WF_E_INVALID; WF_E_UNSUPPORTED for a call of 2^23 workgroups of 16
- * rows or more.
+ * rows or more, and for a larger max_visible.
  */
 int wf_cache_attend(wf_cache_t cache, int32_t precision, const wf_rows *q, const wf_rows *out, int32_t B, int32_t n,
                     int32_t q_heads, const int32_t *table, int32_t table_pages, const int32_t *visible,

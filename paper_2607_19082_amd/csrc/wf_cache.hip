@@ -427,6 +427,8 @@ int wf_cache_attend(wf_cache_t cache, int32_t precision, const wf_rows* q, const
     if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(WF_E_INVALID, "scale must be positive and finite");
     if (max_visible < 0 || max_visible > (long long)table_pages << c->c.page_shift)
         return fail(WF_E_INVALID, "max_visible must lie in [0, table_pages * page]");
+    // the kernel counts tokens in 32 bits, up to the end of the last one's tile and the next
+    if (max_visible > INT32_MAX - 2 * kKvTile) return fail(WF_E_UNSUPPORTED, "max_visible is beyond 2^31 - 65");
     if (mask && !mask_stride) return fail(WF_E_INVALID, "mask_stride is NULL");
     if (!B || !n) return WF_OK;
     if (!visible || (max_visible && !table)) return fail(WF_E_INVALID, "visible or table is NULL");

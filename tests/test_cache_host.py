@@ -95,6 +95,19 @@ assert made and all(c.stream == 0x77 for c in made) and made[-1].what == SYNC
 ''')
 
 
+def test_token_counts_stay_in_32_bits(run):
+    """Calls whose last tiles would end past 2^31 tokens are refused before
+    anything is launched; the longest that fits is not."""
+    run(r'''
+h, _ = plan(1, 64, 4, 1024)
+for most in (2**31 - 1, 2**31 - 32, 2**31 - 64):
+    rc, made = attend(h, 1, 1, 1, most, pages=1 << 21)
+    assert rc == wf.WF_E_UNSUPPORTED and not made, most
+assert attend(h, 1, 1, 1, 2**31 - 65, pages=1 << 21)[0] == 0
+assert attend(h, 1, 1, 1, 2**31 - 1, pages=1 << 20)[0] == wf.WF_E_INVALID      # more than the table holds
+''')
+
+
 def test_the_bindings_sync_waits_for_the_caches_device():
     """Cache.sync without a stream waits for the current stream of the cache's
     device, as the calls use it."""
