@@ -467,7 +467,9 @@ class Cache:
     (contiguous; sequence, token and head may have any strides) and contiguous
     int32 elsewhere.  Calls are asynchronous on the given (default: that device's
     current) torch stream, whatever device is current; one attend call in flight
-    per cache.  sync() waits and raises what a kernel found wrong."""
+    per cache.  A stream that is given has to wait for what the inputs come from,
+    as for any torch call; memory that it uses is kept for it.  sync() waits and
+    raises what a kernel found wrong."""
 
     def __init__(self, heads, dim, pages, page=64):
         import torch
@@ -524,14 +526,27 @@ class Cache:
 
     def _new(self, shape, dtype, stream, like=None):
         """A contiguous tensor and its rows."""
-        t = self._empty(shape, dtype=dtype, device=self._device) if like is None else self._empty_like(like)
-        if stream is not None:          # allocated on the current stream, used on another
-            t.record_stream(stream)
+        if stream is None:
+            t = self._empty(shape, dtype=dtype, device=self._device) if like is None else self._empty_like(like)
+        else:
+            # memory of the stream that writes it: what the current stream has
+            # let go of may still be in use there
+            import torch
+            with torch.cuda.stream(stream):
+                t = self._empty(shape, dtype=dtype, device=self._device)
+            t.record_stream(torch.cuda.current_stream(self._device))
         _, n, heads, dim = shape
         return t, _pack_rows(t.data_ptr(), n * heads * dim, heads * dim, dim)
 
-    def _stream(self, stream):
-        return self._current(self._device) if stream is None else stream.cuda_stream
+    def _stream(self, stream, *used):
+        """The handle of a call's stream.  Tensors used on another stream than
+        the current one keep their memory until that has passed the call."""
+        if stream is None:
+            return self._current(self._device)
+        for t in used:
+            if t is not None:
+                t.record_stream(stream)
+        return stream.cuda_stream
 
     def write(self, k, v, table, first, counts=None, stream=None):
         """Quantise k and v [B][n][heads][dim] into the cache: token i of
@@ -545,7 +560,7 @@ class Cache:
         rc = self._lib.wf_cache_write(
             self._h, self._type(dtype), self._rows(k, shape, dtype, "k"), self._rows(v, shape, dtype, "v"), B, n, p_table,
             pages, self._ints(first, (B,), "first"), None if counts is None else self._ints(counts, (B,), "counts"),
-            self._stream(stream))
+            self._stream(stream, k, v, table, first, counts))
         if rc:
             _check(rc)
 
@@ -568,7 +583,7 @@ class Cache:
             k_rows, v_rows = self._rows(k, shape, dtype, "k"), self._rows(v, shape, dtype, "v")
         rc = self._lib.wf_cache_read(
             self._h, precision, k_rows, v_rows, B, n, p_table, pages, self._ints(first, (B,), "first"),
-            None if counts is None else self._ints(counts, (B,), "counts"), self._stream(stream))
+            None if counts is None else self._ints(counts, (B,), "counts"), self._stream(stream, k, v, table, first, counts))
         if rc:
             _check(rc)
         return k, v
@@ -604,7 +619,8 @@ class Cache:
             p_mask, strides = mask.data_ptr(), (ctypes.c_int64 * 2)(mask.stride(0), mask.stride(1))
         rc = self._lib.wf_cache_attend(
             self._h, precision, q_rows, out_rows, B, n, hq, p_table, pages, self._ints(visible, (B, n), "visible"),
-            p_mask, strides, max_visible, self.dim ** -0.5 if scale is None else scale, self._stream(stream))
+            p_mask, strides, max_visible, self.dim ** -0.5 if scale is None else scale,
+            self._stream(stream, q, table, visible, mask, out))
         if rc:
             _check(rc)
         return out
