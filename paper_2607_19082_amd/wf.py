@@ -73,6 +73,12 @@ Rows = ctypes.c_int64 * 4
 _pack_rows = struct.Struct("4q").pack
 
 
+def _sizes(*sizes):
+    """Refuses what ctypes would cut down to 32 bits."""
+    if not -1 << 31 <= min(sizes) <= max(sizes) < 1 << 31:
+        raise ValueError(f"sizes do not fit 32 bits: {sizes}")
+
+
 class Out(ctypes.Structure):
     _fields_ = [
         ("y_hat", ctypes.c_void_p), ("mean", ctypes.c_void_p), ("scale", ctypes.c_void_p),
@@ -473,6 +479,7 @@ class Cache:
 
     def __init__(self, heads, dim, pages, page=64):
         import torch
+        _sizes(heads, dim, pages, page)
         h = ctypes.c_void_p()
         _check(lib().wf_cache_plan(ctypes.byref(CacheDesc(heads, dim, pages, page)), ctypes.byref(h)))
         self._h = h
@@ -557,6 +564,8 @@ class Cache:
         B, n = shape[0], shape[1]
         shape = (B, n, self.heads, self.dim)
         p_table, pages = self._table(table, B)
+        if (B | n | pages) >> 31:
+            _sizes(B, n, pages)
         rc = self._lib.wf_cache_write(
             self._h, self._type(dtype), self._rows(k, shape, dtype, "k"), self._rows(v, shape, dtype, "v"), B, n, p_table,
             pages, self._ints(first, (B,), "first"), None if counts is None else self._ints(counts, (B,), "counts"),
@@ -570,6 +579,8 @@ class Cache:
         written to the pair `out`.  Tokens past counts[b] are zeros."""
         B = table.shape[0]
         p_table, pages = self._table(table, B)
+        if (B | n | pages) >> 31:
+            _sizes(B, n, pages)
         shape = (B, n, self.heads, self.dim)
         if out is None:
             dtype = self._float if dtype is None else dtype
@@ -605,6 +616,8 @@ class Cache:
         p_table, pages = self._table(table, B)
         if max_visible is None:
             max_visible = pages * self.page if mask is None else mask.shape[-1]
+        if (B | n | hq | pages | max_visible) >> 31:
+            _sizes(B, n, hq, pages, max_visible)
         if out is None:
             out, out_rows = self._new(shape, dtype, stream, like=q if q.is_contiguous() else None)
         else:

@@ -67,3 +67,10 @@ def test_null_arguments(lib):
     assert lib.wf_cache_attend(None, 0, r, r, 1, 1, 1, None, 1, None, None, None, 1, 1.0, None) == wf.WF_E_INVALID
     assert lib.wf_cache_sync(None, None) == wf.WF_E_INVALID
     lib.wf_cache_destroy(None)
+
+
+@pytest.mark.parametrize("desc", [(1, 64, (1 << 32) + 1, 64), ((1 << 32) + 1, 64, 1, 64), (1, 64 - (1 << 32), 1, 64), (1, 64, 1, (1 << 33) + 64)])
+def test_sizes_beyond_32_bits_are_refused(lib, desc):
+    """ctypes would cut them down to sizes that are fine."""
+    with pytest.raises(ValueError):
+        wf.Cache(*desc)

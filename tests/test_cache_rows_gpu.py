@@ -195,3 +195,21 @@ def test_bits_of_a_probability(dim, L, sees, dtype):
     got, bar = cp.misses(dtype, out[0].float().cpu().numpy(), ref, mag)
     assert got <= bar, (got / U, bar / U)
     c.close()
+
+
+# ---- counts that ctypes would cut down --------------------------------------------------
+
+
+def test_counts_beyond_32_bits_are_refused():
+    c, table = filled(torch.ones((1, 3, 1, 64)), torch.ones((1, 3, 1, 64)))
+    q, vis = torch.ones((1, 1, 1, 64), device="cuda"), ints([[3]])
+    for most in (1 << 32, (1 << 32) + 3, 3 - (1 << 32)):
+        with pytest.raises(ValueError):
+            c.attend(q, table, vis, max_visible=most)
+    many = torch.ones((1, 1, 1, 64), device="cuda").expand(1, (1 << 32) + 1, 1, 64)
+    with pytest.raises(ValueError):
+        c.write(many, many, table, ints([0]))
+    with pytest.raises(ValueError):
+        c.read(table, ints([0]), (1 << 32) + 1, out=(many, many))
+    assert (c.attend(q, table, vis, max_visible=3) == 1).all()
+    c.close()
