@@ -515,7 +515,7 @@ typedef struct {
 } wf_rows;
 
 /* Build a cache: the pool (zeros: a token that was never written reads as 0)
- * and the workspace of its attention calls (64 Ki rows of dim + 2 floats).
+ * and the workspace of its attention calls (5 MB, or 21 MB for dim above 64).
  * Synchronous; uses the current HIP device, on which all its calls run, whatever
  * device is current for them (a stream of theirs is that device's; NULL: its
  * default stream).

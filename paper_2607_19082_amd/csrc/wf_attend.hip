@@ -52,11 +52,6 @@ typedef unsigned u2 __attribute__((ext_vector_type(2)));
 // read-only for the whole launch, at addresses that a wave shares: scalar loads
 typedef const int __attribute__((address_space(4))) * SharedInts;
 
-// Workgroups that a call is split into: one for each compute unit.  us for 192
-// / 256 / 320 / 512: one token over 131072 35 / 33 / 40 / 34; 45 fp32 rows over
-// 32300 17 / 14 / 19 / 16; 56 fp32 rows of 256 channels over 20011 28 / 24 / 34
-// / 30 (the last ones wait for a place, and the join has more to read).
-constexpr int kAtTarget = 256;
 constexpr int kAtMaxSplits = 256;
 constexpr int kAtJoin = 256;        // threads of the kernel that joins the splits
 // Waves of a workgroup.  (16 instead of 8: 9.0 against 8.1 us for a token over
@@ -748,8 +743,6 @@ long long attend_plan(AttendArgs& a, int precision) {
         if (!s && groups <= kAtTarget * 5 / 4) s = 4;
     }
     s = s < by_len ? s : by_len;
-    const long long by_room = kAttendWorkRows / (groups * 16 * nt);
-    s = s < by_room ? s : by_room;
     s = s < kAtMaxSplits ? s : kAtMaxSplits;
     a.splits = s < 2 ? 1 : (int)s;
     a.splits_.by(a.splits);

@@ -43,8 +43,17 @@ constexpr int kKvMaxPower = 125;     // powers lie in 2^-125 .. 2^125: every val
 // device error word: a token or row past the page table, a table entry outside the pool
 constexpr int kErrKvRange = 1, kErrKvPage = 2;
 
-// rows of partial results that a cache's workspace holds (see attend_plan)
-constexpr long long kAttendWorkRows = 1 << 16;
+// Workgroups that a call is split into: one for each compute unit.  us for 192
+// / 256 / 320 / 512: one token over 131072 35 / 33 / 40 / 34; 45 fp32 rows over
+// 32300 17 / 14 / 19 / 16; 56 fp32 rows of 256 channels over 20011 28 / 24 / 34
+// / 30 (the last ones wait for a place, and the join has more to read).
+constexpr int kAtTarget = 256;
+// Rows of partial results that a cache's workspace holds: what attend_plan's
+// calls can take.  At most 2 kAtTarget workgroups share calls of up to kAtTarget
+// of them, and four each a quarter more; they have 32 rows for 128 channels in
+// bf16, else 16 (64 channels have 32 from 512 workgroups on, which no call that
+// is split has).
+inline size_t attend_work_rows(int dp) { return (size_t)4 * (kAtTarget * 5 / 4) * (dp == 128 ? 32 : 16); }
 
 // n / d for n < 2^31 by a product: with 2^l the power from d up, mul =
 // floor(2^(31 + l) / d) + 1 is off by less than 2^(31 + l) / (d n).  (The
@@ -166,8 +175,7 @@ struct AttendArgs {
 
 void launch_kv_write(const KvCache&, int precision, const KvRows& k, const KvRows& v, const KvTokens&, hipStream_t);
 void launch_kv_read(const KvCache&, int precision, const KvRows& k, const KvRows& v, const KvTokens&, hipStream_t);
-// The splits of a call, so that its partial results fit the workspace.  Returns
-// the threads of its launch.
+// The splits of a call.  Returns the threads of its launch.
 long long attend_plan(AttendArgs&, int precision);
 void launch_attend(const AttendArgs&, int precision, hipStream_t);
 

@@ -353,7 +353,7 @@ int wf_cache_plan(const wf_cache_desc* d, wf_cache_t* out) try {
     while ((1 << k.page_shift) < d->page) ++k.page_shift;
     // (a record is a multiple of 64 bytes)
     const size_t head = kKvHead, pool = (k.page_bytes() * k.pages + 255) / 256 * 256;
-    const size_t work = (size_t)kAttendWorkRows * (k.dp + 2) * sizeof(float);
+    const size_t work = attend_work_rows(k.dp) * (k.dp + 2) * sizeof(float);
     hipError_t e = hipGetDevice(&c->device);
     if (e != hipSuccess) {
         free_cache(c);
@@ -445,7 +445,7 @@ int wf_cache_attend(wf_cache_t cache, int32_t precision, const wf_rows* q, const
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     if (attend_plan(a, precision) >= 1LL << 32) return fail(WF_E_UNSUPPORTED, "2^32 or more threads in one call");
     a.part_o = c->work;
-    a.part_ml = c->work + (size_t)kAttendWorkRows * c->c.dp;
+    a.part_ml = c->work + attend_work_rows(c->c.dp) * c->c.dp;
     const OnDevice on(c->device);
     if (on.error() != hipSuccess) return kv_fail(on.error(), "the cache's device");
     launch_attend(a, precision, stream);

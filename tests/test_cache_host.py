@@ -108,6 +108,27 @@ assert attend(h, 1, 1, 1, 2**31 - 1, pages=1 << 20)[0] == wf.WF_E_INVALID      #
 ''')
 
 
+def test_workspace_is_what_calls_take(run):
+    """Partial results of split calls, over the workgroups and lengths that the
+    split follows from, fit the workspace, and one of them fills it."""
+    run(r'''
+for dim in (64, 128, 256):
+    h, held = plan(1, dim, 64, 64)
+    room = held - 256 - 64 * 64 * dim * 17 // 16
+    most = 0
+    for precision in (0, 1):
+        item = 4 - 2 * precision
+        for n in list(range(1, 34)) + list(range(48, 340 * 32, 16)):
+            for length in (100, 300, 1000, 2100, 8191, 8192, 30000, 131072, 1 << 21):
+                rc, made = attend(h, 1, n, 1, length, precision=precision)
+                assert rc == 0 and len(made) in (1, 2)
+                if len(made) == 2:
+                    two = made[0].block == 256 and dim * item < 1024
+                    most = max(most, made[0].grid * 16 * (2 if two else 1) * (dim + 2) * 4)
+    assert most == room, (dim, most, room)
+''')
+
+
 def test_the_bindings_sync_waits_for_the_caches_device():
     """Cache.sync without a stream waits for the current stream of the cache's
     device, as the calls use it."""
