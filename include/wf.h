@@ -565,12 +565,13 @@ int wf_cache_read(wf_cache_t cache, int32_t precision, const wf_rows *k, const w
  *                WF_E_CAPACITY
  *   scale        positive; 1 / sqrt(dim) as a rule
  * Tokens in a page outside the pool are left out, and the next wf_cache_sync
- * returns WF_E_INVALID.  Sums are held in fp32, before they are divided (they
- * overflow where |v| is beyond about 2^112 / the row's tokens).  Their order
- * follows from the call's sizes and, since rows are taken in tiles, from the
- * visible counts of the rows that share one: the same call gives the same bits,
- * whatever lies at tokens that a row does not see.  Asynchronous on `stream`;
- * one call in flight per cache (the workspace is shared by its calls).
+ * returns WF_E_INVALID.  Scores (times log2 e) and sums are held in fp32, the
+ * sums before they are divided: they overflow where |v| is beyond about 2^112 /
+ * the row's tokens.  The order of a sum follows from the call's sizes and, since
+ * rows are taken in tiles, from the visible counts of the rows that share one:
+ * the same call gives the same bits, whatever lies at tokens that a row does not
+ * see.  Asynchronous on `stream`; one call in flight per cache (the workspace is
+ * shared by its calls).
  * Errors: WF_E_INVALID; WF_E_UNSUPPORTED for a call of 2^23 workgroups of 16
  * rows or more, and for a larger max_visible.
  */

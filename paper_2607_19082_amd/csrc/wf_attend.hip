@@ -32,7 +32,9 @@
 // where a kernel that only reads reaches 5.7.  A tile costs a wave ~170 vector
 // instructions, 96 of them conversions and the exchange of values between
 // tokens, and 26 products; the two hardly overlap, so with many rows (1024
-// queries, 32 heads, 16384 tokens: 343 us, 0.78 PFLOP/s) their sum is the time.
+// queries, 32 heads, 16384 tokens: 350 us, 0.76 PFLOP/s) their sum is the time.
+// In fp32 a tile of 128 channels has 51 products, and one tile of rows a
+// workgroup (the same 1024 queries 643 us, 0.41 PFLOP/s).
 // A short call (a token over 1001: 8 us) is 4 us of launch, loads that wait for
 // each other and the join of the waves, and 1 for each tile of a wave.
 #include <cmath>
@@ -54,8 +56,8 @@ typedef const int __attribute__((address_space(4))) * SharedInts;
 
 constexpr int kAtMaxSplits = 256;
 constexpr int kAtJoin = 256;        // threads of the kernel that joins the splits
-// Waves of a workgroup.  (16 instead of 8: 9.0 against 8.1 us for a token over
-// 1001, 16 against 14.4 for 45 fp32 rows over 32300, since the larger workgroup
+// Waves of a workgroup.  (16 instead of 8: 8.4 against 7.4 us for a token over
+// 1001, 14.6 against 13.8 for 45 fp32 rows over 32300, since the larger workgroup
 // starts later.)
 template <int DP, class T, int NT>
 constexpr int kAtWaves = NT == 1 && DP * sizeof(T) < 1024 ? 8 : 4;
@@ -287,8 +289,8 @@ constexpr int kAtBatch = 256;       // sequences that are taken by length, at mo
 // The sequence that holds a place among all, from the longest down and, past
 // the first `ahead` places, from the shortest up: workgroups of the two halves
 // share a compute unit, and each then has about the same to do.  64 sequences
-// of 0 to 8192 tokens, 8 heads of 128: 60 us, in the order given 67 (of 8192
-// tokens each 110 and 106).
+// of 0 to 8192 tokens, 8 heads of 128: 60 us, in the order given 66 (of 8192
+// tokens each 108 and 105).
 __device__ __forceinline__ int by_length(const AttendArgs& a, int place, int ahead) {
     __shared__ int length[kAtBatch], found;
     const int u = threadIdx.x;
@@ -702,10 +704,10 @@ __global__ __launch_bounds__(kAtJoin) void k_attend_join(AttendArgs a) {
 
 // Column tiles of a workgroup: two, which share a tile's conversions, where they
 // fit the registers and there are enough rows to fill the chip all the same.
-// us with one / two, 8 heads, 8192 tokens: of 128 in bf16, 256 tiles of rows 41
-// / 43, 512 73 / 66, 1024 136 / 111, 2048 262 / 210; of 64 in bf16, 512 50 /
-// 51, 768 70 / 76, 1024 91 / 79; of 64 in fp32, 512 58 / 56, 768 83 / 89, 1024
-// 107 / 94.  Hence tiles times channels.
+// us with one / two, 8 heads, 8192 tokens: of 128 in bf16, 256 tiles of rows 34
+// / 39, 512 64 / 57, 1024 129 / 97, 2048 227 / 190; of 64 in bf16, 512 42 / 45,
+// 768 61 / 67, 1024 76 / 67; of 64 in fp32, 512 54 / 54, 768 80 / 91, 1024 103 /
+// 94.  Hence tiles times channels.
 template <int DP, class T>
 constexpr bool kAtTwoTiles = DP * sizeof(T) <= 256;
 constexpr long long kAtManyRows = 1 << 16;
@@ -722,21 +724,21 @@ long long attend_plan(AttendArgs& a, int precision) {
     const long long groups = (long long)a.B * a.c.heads * ((rows + 16 * nt - 1) / (16 * nt));
     // A tile takes a wave about 1 us and the join 3, so up to four tiles a wave
     // are not split; more are, down to one tile each.  us with no split, four
-    // tiles each, two and one: a token over 1001 (8 heads of 128, bf16) 7.8, 7.8,
-    // 8.6, 7.8, over 2047 11.4, 10.5, 8.6, 7.9, over 8192 33, 10.7, 9.2, 8.6; 45
-    // fp32 rows over 1024 7.1, 7.2, 8.6, 8.0, over 4096 15.5, 10.2, 8.8, 8.5.
+    // tiles each, two and one: a token over 1001 (8 heads of 128, bf16) 7.3, 7.4,
+    // 8.3, 7.4, over 2047 11.0, 10.2, 8.5, 7.8, over 8192 33, 10.6, 9.1, 8.7; 45
+    // fp32 rows over 1024 7.2, 7.2, 8.5, 7.8, over 4096 16.9, 10.7, 9.0, 8.5.
     const long long tiles = ((long long)a.max_visible + kKvTile - 1) / kKvTile;
     const long long by_len = tiles <= 4 * waves ? 1 : (tiles + waves - 1) / waves;
     long long s = kAtTarget / groups;
     // Long calls (8192 tokens) that would leave many compute units idle take two
     // workgroups each where that fills a fifth more: us without and with, 8 key
-    // heads of 128 in bf16, 17 tokens 44 / 38, 11 28 / 25, 18 over 0 to 8192 38 /
-    // 28, 136 tiles of rows 38 / 34; at 4096 tokens 23 / 22, 17 / 17, at 2048
+    // heads of 128 in bf16, 17 tokens 42 / 37, 11 27 / 26, 18 over 0 to 8192 37 /
+    // 29, 136 tiles of rows 33 / 30; at 4096 tokens 24 / 23, 18 / 18, at 2048
     // 13.5 / 16.  A few workgroups more than compute units would take as long as
-    // two each, and are split into four: 33 tokens over 4096 46 / 40, 8192 83 /
-    // 69, 16384 155 / 120, 40 over 8192 86 / 75, 44 86 / 82; 320 tiles of rows
-    // over 4096 37 / 41, 8192 65 / 56, 16384 116 / 90; of 64 channels in fp32 30 /
-    // 36, 52 / 50, 91 / 72; 36 tokens over 0 to 8192 47 / 49, 0 to 16384 88 / 81.
+    // two each, and are split into four: 33 tokens over 4096 44 / 39, 8192 81 /
+    // 67, 16384 156 / 123, 40 over 8192 84 / 74, 44 87 / 82; 320 tiles of rows
+    // over 4096 32 / 35, 8192 59 / 51, 16384 111 / 88; of 64 channels in fp32 29 /
+    // 33, 52 / 46, 99 / 75; 36 tokens over 0 to 8192 46 / 48, 0 to 16384 83 / 80.
     if (tiles >= 256) {
         const long long twice = 2 * kAtTarget / groups;
         if (s && 5 * twice > 12 * s) s = twice;
@@ -749,8 +751,11 @@ long long attend_plan(AttendArgs& a, int precision) {
     a.tiles_.by((unsigned)((rows + 16 * nt - 1) / (16 * nt)));
     a.heads_.by(a.c.heads);
     a.group_.by(a.group);
-    // a token each of sequences that may be of unequal lengths, and two
-    // workgroups on most compute units
+    // A token each of sequences that may be of unequal lengths, and two
+    // workgroups on most compute units.  With more of them the units take the
+    // next as they finish: in the order given and longest first, 128 sequences
+    // of 0 to 8192 tokens 129 / 119 us, but of 8192 each 199 / 207, and 256 of 0
+    // to 8192 226 / 228, of 8192 each 395 / 406.
     const bool two = groups > kAtTarget && groups <= 2 * kAtTarget && bytes <= 256 && a.splits == 1;
     a.ahead = nt == 1 && rows <= 16 && a.B > 1 && a.B <= kAtBatch && two ? (int)(kAtTarget / a.c.heads) : 0;
     return groups * a.splits * waves * 64;

@@ -44,8 +44,8 @@ constexpr int kKvMaxPower = 125;     // powers lie in 2^-125 .. 2^125: every val
 constexpr int kErrKvRange = 1, kErrKvPage = 2;
 
 // Workgroups that a call is split into: one for each compute unit.  us for 192
-// / 256 / 320 / 512: one token over 131072 35 / 33 / 40 / 34; 45 fp32 rows over
-// 32300 17 / 14 / 19 / 16; 56 fp32 rows of 256 channels over 20011 28 / 24 / 34
+// / 256 / 320 / 512: one token over 131072 34 / 33 / 40 / 33; 45 fp32 rows over
+// 32300 16 / 14 / 18 / 15; 56 fp32 rows of 256 channels over 20011 27 / 23 / 35
 // / 30 (the last ones wait for a place, and the join has more to read).
 constexpr int kAtTarget = 256;
 // Rows of partial results that a cache's workspace holds: what attend_plan's

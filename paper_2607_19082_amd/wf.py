@@ -606,7 +606,7 @@ class Cache:
         it allows; a row that sees none gives zeros.  q_heads is a multiple of
         the cache's heads; scale defaults to dim ** -0.5.  max_visible bounds
         visible (default: the mask's width, or all that the table holds; a
-        tighter bound makes a better launch)."""
+        tighter bound makes a better launch).  Outputs carry no gradient."""
         shape, dtype = q.shape, q.dtype
         if len(shape) != 4:
             raise ValueError(f"q: expected four dimensions, got {tuple(shape)}")
