@@ -588,6 +588,62 @@ int wf_cache_sync(wf_cache_t cache, hipStream_t stream);
 /* Release a cache.  NULL is ignored. */
 void wf_cache_destroy(wf_cache_t cache);
 
+/*
+ * Norms of queries and keys for each head, with the position rotation in the
+ * same pass: what an attention context model does to them before they meet the
+ * cache, whose order says nothing of where a latent lies in the grid.  For a head's channels x_c
+ *   y_c = x_c / sqrt(mean_c x_c^2 + eps) * gain_c,
+ * and each pair (a, b) of the first `rotated` channels turns by its position:
+ *   (y_a cos t - y_b sin t, y_a sin t + y_b cos t),  t = position * frequency.
+ * With two axes (row and column), the first half of the rotated channels turns
+ * by the first, the second half by the second, both with the same frequencies.
+ */
+typedef enum {
+    WF_PAIRS_HALVES = 0,    /* channel j of an axis with channel j + half of that axis's channels */
+    WF_PAIRS_NEIGHBOURS = 1 /* channel 2 j with channel 2 j + 1                                   */
+} wf_pairs;
+
+typedef struct {
+    int32_t dim;            /* channels of a head: a multiple of 8 in [8, 256]              */
+    int32_t rotated;        /* channels that turn, a head's first: a multiple of 8 axes; 0: none */
+    int32_t axes;           /* 1: a position, 2: two                                        */
+    int32_t pairs;          /* wf_pairs                                                     */
+    float eps;              /* positive, not subnormal                                      */
+    const double *frequencies; /* HOST, rotated / (2 axes) radians a position, each within a turn
+                               (2 pi) of 0; copied.  NULL where rotated is 0                */
+} wf_head_norm_desc;
+
+typedef struct wf_head_norm_s *wf_head_norm_t;
+
+/* Host only but for the current HIP device, on which all its calls run, whatever
+ * device is current for them.  A call takes what it needs of the plan, so that a
+ * captured one does without it.  Errors: WF_E_INVALID, WF_E_UNSUPPORTED,
+ * WF_E_NOMEM, WF_E_HIP. */
+int wf_head_norm_plan(const wf_head_norm_desc *desc, wf_head_norm_t *out);
+
+/*
+ *   q, q_out     [B][n][q_heads][dim] rows, fp32 or bf16 as the precision says
+ *   k, k_out     [B][n][k_heads][dim], of the same precision; k_heads 0: none
+ *   q_gain, k_gain  [dim] DEVICE fp32 for all heads, or NULL: ones
+ *   positions    [B][n][axes] DEVICE int32, any values; may be NULL where nothing
+ *                is rotated
+ *   counts       NULL, or [B] DEVICE int32: token i of sequence b is taken where
+ *                i < counts[b]; the others' outputs are left as they were
+ * Outputs may be the inputs (the same rows, in place); otherwise they must not
+ * overlap with any input.  Sums of squares are held in 64 bits, the rest in
+ * fp32, each output rounded once; an angle is exact to 2^-31 of a turn at any
+ * position.  A head's bits depend on its channels, gain and position alone.
+ * Asynchronous on `stream`; any number of calls of a plan may be in flight.
+ * Errors: WF_E_INVALID; WF_E_UNSUPPORTED for 2^31 tokens or more, more than
+ * 65536 heads of either, or a launch of 2^32 threads.
+ */
+int wf_head_norm(wf_head_norm_t plan, int32_t precision, const wf_rows *q, const wf_rows *q_out, int32_t q_heads,
+                 const float *q_gain, const wf_rows *k, const wf_rows *k_out, int32_t k_heads, const float *k_gain,
+                 int32_t B, int32_t n, const int32_t *positions, const int32_t *counts, hipStream_t stream);
+
+/* Release a plan.  NULL is ignored. */
+void wf_head_norm_destroy(wf_head_norm_t plan);
+
 /* Release everything the plan owns.  NULL is ignored. */
 void wf_plan_destroy(wf_plan_t plan);
 

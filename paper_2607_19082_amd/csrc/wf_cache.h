@@ -32,7 +32,7 @@
 
 #include <cstdint>
 
-#include "wf_internal.h"
+#include "wf_call.h"
 
 namespace wf {
 
@@ -145,11 +145,6 @@ struct KvLayout {
         return 16 * DP + piece(t / 8 * 16 + d / kRows, t % 8 * kUnit + d % kRows / 2);
     }
     __device__ static int value_power(int t, int block) { return value_powers(block) + t; }
-};
-
-struct KvRows {                      // [b][row][head][dim], the channels contiguous
-    void* p;
-    long long sb, sr, sh;            // strides in elements
 };
 
 struct KvTokens {                    // the tokens a write or read takes

@@ -267,45 +267,10 @@ struct Cache {
     float* work = nullptr;           // partial results of split attention calls
 };
 
-static int kv_fail(hipError_t e, const char* what) { return fail(WF_E_HIP, std::string(what) + ": " + hipGetErrorString(e)); }
-
-// Makes a cache's device current for a call.  A default stream is that of the
-// current device, and a host thread may have another one current (a new thread
-// begins with device 0).
-class OnDevice {
-public:
-    explicit OnDevice(int device) {
-        e_ = hipGetDevice(&was_);
-        if (e_ == hipSuccess && was_ != device) {
-            e_ = hipSetDevice(device);
-            changed_ = e_ == hipSuccess;
-        }
-    }
-    ~OnDevice() {
-        if (changed_) (void)hipSetDevice(was_);
-    }
-    OnDevice(const OnDevice&) = delete;
-    OnDevice& operator=(const OnDevice&) = delete;
-    hipError_t error() const { return e_; }
-
-private:
-    int was_ = 0;
-    bool changed_ = false;
-    hipError_t e_;
-};
-
 static void free_cache(Cache* c) {
     if (!c) return;
     if (c->memory) (void)hipFree(c->memory);
     delete c;
-}
-
-// Rows of a call: the strides are in elements and the channels contiguous.
-static int kv_rows(const wf_rows* r, int precision, const char* name, KvRows* out) {
-    if (!r || !r->data) return fail(WF_E_INVALID, std::string(name) + " is NULL");
-    if ((uintptr_t)r->data % (precision == WF_BF16 ? 2 : 4)) return fail(WF_E_INVALID, std::string(name) + " is not aligned to its element");
-    *out = {r->data, r->stride[0], r->stride[1], r->stride[2]};
-    return WF_OK;
 }
 
 static int kv_tokens(const Cache* c, int precision, int B, int n, const int32_t* table, int table_pages, const int32_t* first,
@@ -321,11 +286,6 @@ static int kv_tokens(const Cache* c, int precision, int B, int n, const int32_t*
     out->heads_.by(c->c.heads);
     out->records_.by((unsigned)records);
     return WF_OK;
-}
-
-static int kv_launched(const char* what) {
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? WF_OK : kv_fail(e, what);
 }
 
 }  // namespace wf

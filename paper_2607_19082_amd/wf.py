@@ -20,13 +20,14 @@ MASK = {"full": 0, "relaxed": 1, "3x3": 2, "7x7": 3}
 PARAM_ORDER = {"native": 0, "scales_first": 1}
 KERNEL = {"full": 5, "relaxed": 5, "3x3": 3, "7x7": 7}   # ctx_w's spatial size per mask
 PRECISION = {"fp32": 0, "bf16": 1}
+PAIRS = {"halves": 0, "neighbours": 1}
 DRIVER = {"stream": 0, "graph": 1, "persistent": 2, "dataflow": 3, "resident": 4}
 
 EXPORTS = ["wf_schedule", "wf_validate", "wf_plan", "wf_plan_schedule", "wf_plan_deps", "wf_plan_set_waits", "wf_litmus", "wf_decode",
            "wf_encode", "wf_ec_tables", "wf_mix_tables", "wf_encode_bits", "wf_decode_bits", "wf_plan_trace",
            "wf_measure_floor", "wf_plan_sync", "wf_xform_plan", "wf_hyper_synthesis", "wf_synthesis",
            "wf_decode_noalloc", "wf_cache_plan", "wf_cache_write", "wf_cache_read", "wf_cache_attend", "wf_cache_sync",
-           "wf_cache_destroy", "wf_xform_destroy", "wf_plan_destroy", "wf_last_error"]
+           "wf_cache_destroy", "wf_head_norm_plan", "wf_head_norm", "wf_head_norm_destroy", "wf_xform_destroy", "wf_plan_destroy", "wf_last_error"]
 
 
 class WfError(RuntimeError):
@@ -65,6 +66,11 @@ class XformDesc(ctypes.Structure):
 class CacheDesc(ctypes.Structure):
     _fields_ = [("heads", ctypes.c_int32), ("dim", ctypes.c_int32), ("pages", ctypes.c_int32),
                 ("page", ctypes.c_int32)]
+
+
+class HeadNormDesc(ctypes.Structure):
+    _fields_ = [("dim", ctypes.c_int32), ("rotated", ctypes.c_int32), ("axes", ctypes.c_int32), ("pairs", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("frequencies", ctypes.c_void_p)]
 
 
 # wf_rows: a pointer and three strides, as four words (an array of them, or
@@ -121,6 +127,9 @@ def lib():
         L.wf_cache_read.argtypes = [P, i32, P, P, i32, i32, P, i32, P, P, P]
         L.wf_cache_attend.argtypes = [P, i32, P, P, i32, i32, i32, P, i32, P, P, P, i32, ctypes.c_float, P]
         L.wf_cache_sync.argtypes = [P, P]
+        L.wf_head_norm_plan.argtypes = [ctypes.POINTER(HeadNormDesc), ctypes.POINTER(ctypes.c_void_p)]
+        L.wf_head_norm.argtypes = [P, i32, P, P, i32, P, P, P, i32, P, i32, i32, P, P, P]
+        L.wf_head_norm_destroy.argtypes = [P]
         L.wf_cache_destroy.argtypes = [P]
         L.wf_plan_trace.argtypes = [P, P, ctypes.c_int64, P, P]
         L.wf_measure_floor.argtypes = [P, P, P]
@@ -132,6 +141,7 @@ def lib():
             getattr(L, name).restype = ctypes.c_int
         L.wf_xform_destroy.restype = None
         L.wf_cache_destroy.restype = None
+        L.wf_head_norm_destroy.restype = None
         _lib = L
     return _lib
 
@@ -461,30 +471,14 @@ class Xform:
         return image
 
 
-class Cache:
-    """A key/value cache held in 4 bits, in pages, and the attention over it
-    (wf_cache_*; the format is described there).
+class _TokenCalls:
+    """What the classes whose calls take rows of tokens have in common: checks of
+    tensors, new ones, and a call's stream.  Their calls run on the device that
+    was current when they were made."""
 
-    heads, dim   key heads and channels of a head (a multiple of 8, up to 256)
-    pages, page  pages of the pool, tokens of a page (a power of two, 32 to 1024)
-
-    Token t of sequence b lies in page table[b, t // page].  Tensors are torch
-    tensors on the HIP device that was current at the plan, fp32 or bf16 where they hold channels
-    (contiguous; sequence, token and head may have any strides) and contiguous
-    int32 elsewhere.  Calls are asynchronous on the given (default: that device's
-    current) torch stream, whatever device is current; one attend call in flight
-    per cache.  A stream that is given has to wait for what the inputs come from,
-    as for any torch call; memory that it uses is kept for it.  sync() waits and
-    raises what a kernel found wrong."""
-
-    def __init__(self, heads, dim, pages, page=64):
+    def _on_device(self):
         import torch
-        _sizes(heads, dim, pages, page)
-        h = ctypes.c_void_p()
-        _check(lib().wf_cache_plan(ctypes.byref(CacheDesc(heads, dim, pages, page)), ctypes.byref(h)))
-        self._h = h
         self._device = torch.cuda.current_device()
-        self.heads, self.dim, self.pages, self.page = heads, dim, pages, page
         # a serving step makes several short calls: what they look up is kept
         self._lib = lib()
         self._int, self._float, self._bool, self._empty, self._empty_like = \
@@ -493,17 +487,6 @@ class Cache:
         # the handle of a device's current stream, without a Stream object
         self._current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda device: torch.cuda.current_stream(device).cuda_stream)
-
-    def close(self):
-        if getattr(self, "_h", None):
-            lib().wf_cache_destroy(self._h)
-            self._h = None
-
-    def __del__(self):
-        try:
-            self.close()
-        except Exception:
-            pass
 
     def _rows(self, t, shape, dtype, name):
         if t.dtype is dtype and t.shape == shape and t.get_device() == self._device:
@@ -524,12 +507,6 @@ class Cache:
         if precision is None:
             raise ValueError(f"expected torch.float32 or torch.bfloat16, got {dtype}")
         return precision
-
-    def _table(self, table, B):
-        shape = table.shape
-        if len(shape) != 2:
-            raise ValueError(f"table: expected two dimensions, got {tuple(shape)}")
-        return self._ints(table, (B, shape[1]), "table"), shape[1]
 
     def _new(self, shape, dtype, stream, like=None):
         """A contiguous tensor and its rows."""
@@ -554,6 +531,48 @@ class Cache:
             if t is not None:
                 t.record_stream(stream)
         return stream.cuda_stream
+
+
+class Cache(_TokenCalls):
+    """A key/value cache held in 4 bits, in pages, and the attention over it
+    (wf_cache_*; the format is described there).
+
+    heads, dim   key heads and channels of a head (a multiple of 8, up to 256)
+    pages, page  pages of the pool, tokens of a page (a power of two, 32 to 1024)
+
+    Token t of sequence b lies in page table[b, t // page].  Tensors are torch
+    tensors on the HIP device that was current at the plan, fp32 or bf16 where they hold channels
+    (contiguous; sequence, token and head may have any strides) and contiguous
+    int32 elsewhere.  Calls are asynchronous on the given (default: that device's
+    current) torch stream, whatever device is current; one attend call in flight
+    per cache.  A stream that is given has to wait for what the inputs come from,
+    as for any torch call; memory that it uses is kept for it.  sync() waits and
+    raises what a kernel found wrong."""
+
+    def __init__(self, heads, dim, pages, page=64):
+        _sizes(heads, dim, pages, page)
+        h = ctypes.c_void_p()
+        _check(lib().wf_cache_plan(ctypes.byref(CacheDesc(heads, dim, pages, page)), ctypes.byref(h)))
+        self._h = h
+        self._on_device()
+        self.heads, self.dim, self.pages, self.page = heads, dim, pages, page
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib().wf_cache_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _table(self, table, B):
+        shape = table.shape
+        if len(shape) != 2:
+            raise ValueError(f"table: expected two dimensions, got {tuple(shape)}")
+        return self._ints(table, (B, shape[1]), "table"), shape[1]
 
     def write(self, k, v, table, first, counts=None, stream=None):
         """Quantise k and v [B][n][heads][dim] into the cache: token i of
@@ -640,3 +659,102 @@ class Cache:
 
     def sync(self, stream=None):
         _check(self._lib.wf_cache_sync(self._h, self._stream(stream)))
+
+
+class HeadNorm(_TokenCalls):
+    """Norms of queries and keys for each head, with the position rotation in the
+    same pass (wf_head_norm):
+      y_c = x_c / sqrt(mean_c x_c^2 + eps) * gain_c, and each pair of the first
+      `rotated` channels turned by position * frequency.
+
+    dim          channels of a head (a multiple of 8, up to 256)
+    rotated      channels that turn (default: all; a multiple of 8 axes; 0: none)
+    axes         1: a position a token, 2: two (row and column; the first half of
+                 the rotated channels turns by the first, the rest by the second)
+    pairs        "halves": channel j with the one half of an axis's channels on;
+                 "neighbours": channels 2 j and 2 j + 1
+    frequencies  radians a position, one for each pair of an axis (default:
+                 base ** (-j / pairs of an axis))
+
+    Devices and streams as for Cache; any number of calls may be in flight."""
+
+    def __init__(self, dim, eps=1e-6, base=10000.0, rotated=None, axes=1, pairs="halves", frequencies=None):
+        rotated = dim if rotated is None else rotated
+        _sizes(dim, rotated, axes)
+        each = rotated // (2 * axes) if axes > 0 else 0
+        if frequencies is None:
+            frequencies = float(base) ** (-np.arange(max(0, each), dtype=np.float64) / max(1, each))
+        f = np.ascontiguousarray(frequencies, dtype=np.float64)
+        if f.shape != (max(0, each),):
+            raise ValueError(f"frequencies must have shape ({each},), got {f.shape}")
+        h = ctypes.c_void_p()
+        d = HeadNormDesc(dim, rotated, axes, PAIRS[pairs], eps, f.ctypes.data)
+        _check(lib().wf_head_norm_plan(ctypes.byref(d), ctypes.byref(h)))
+        self._h = h
+        self._on_device()
+        self.dim, self.rotated, self.axes = dim, rotated, axes
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib().wf_head_norm_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _gain(self, t, name):
+        if t.dtype is self._float and t.shape == (self.dim,) and t.get_device() == self._device and t.is_contiguous():
+            return t.data_ptr()
+        raise ValueError(f"{name}: expected a contiguous fp32 tensor ({self.dim},) on device {self._device}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+
+    def apply(self, q, positions, k=None, q_gain=None, k_gain=None, counts=None, out=None, stream=None):
+        """Normed and rotated q [B][n][q_heads][dim], and k [B][n][k_heads][dim] of
+        the same type where it is given: a new tensor (with k a pair), or written
+        to `out` (a tensor or pair), which may be the inputs.  positions is int32
+        [B][n], with two axes [B][n][2] (None where nothing is rotated); gains are
+        fp32 [dim] (None: ones).  With counts (int32 [B]) tokens from counts[b] on
+        are left as they were in `out` (a new tensor holds anything there).
+        Outputs carry no gradient."""
+        shape, dtype = q.shape, q.dtype
+        if len(shape) != 4:
+            raise ValueError(f"q: expected four dimensions, got {tuple(shape)}")
+        B, n, hq, _ = shape
+        precision = self._type(dtype)
+        q_shape, hk, k_rows, ko_rows, p_k_gain = (B, n, hq, self.dim), 0, None, None, None
+        q_rows = self._rows(q, q_shape, dtype, "q")
+        if k is not None:
+            if len(k.shape) != 4:
+                raise ValueError(f"k: expected four dimensions, got {tuple(k.shape)}")
+            hk = k.shape[2]
+            k_shape = (B, n, hk, self.dim)
+            k_rows = self._rows(k, k_shape, dtype, "k")
+            if k_gain is not None:
+                p_k_gain = self._gain(k_gain, "k_gain")
+        if (B | n | hq | hk) >> 31:
+            _sizes(B, n, hq, hk)
+        if out is None:
+            qo, qo_rows = self._new(q_shape, dtype, stream, like=q if q.is_contiguous() else None)
+            ko = None
+            if k is not None:
+                ko, ko_rows = self._new(k_shape, dtype, stream, like=k if k.is_contiguous() else None)
+        else:
+            qo, ko = (out, None) if k is None else out
+            qo_rows = self._rows(qo, q_shape, dtype, "out")
+            if k is not None:
+                ko_rows = self._rows(ko, k_shape, dtype, "out")
+        p_positions = None
+        if self.rotated and positions is None:
+            raise ValueError("positions: needed where channels are rotated")
+        if positions is not None:
+            p_positions = self._ints(positions, (B, n) if self.axes == 1 else (B, n, 2), "positions")
+        rc = self._lib.wf_head_norm(
+            self._h, precision, q_rows, qo_rows, hq, None if q_gain is None else self._gain(q_gain, "q_gain"), k_rows, ko_rows,
+            hk, p_k_gain, B, n, p_positions, None if counts is None else self._ints(counts, (B,), "counts"),
+            self._stream(stream, q, k, positions, q_gain, k_gain, counts, qo, ko))
+        if rc:
+            _check(rc)
+        return qo if k is None else (qo, ko)
