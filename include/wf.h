@@ -580,6 +580,46 @@ int wf_cache_attend(wf_cache_t cache, int32_t precision, const wf_rows *q, const
                     const uint8_t *mask, const int64_t *mask_stride, int32_t max_visible, float scale,
                     hipStream_t stream);
 
+/*
+ * The same attention with a sliding window and a few first tokens that stay
+ * visible: of the tokens j < visible[b][i], a row sees those with
+ *   j >= visible[b][i] - window  or  j < sinks.
+ * Pages that hold none of them are not read, and their table entries need not
+ * be in the pool: a caller may give them to other sequences.  The time goes by
+ * window and sinks, not by the sequence.
+ *   window       positive (a row's own token counts where it is in the cache)
+ *   sinks        not negative
+ * The rest, the errors among it, as for wf_cache_attend without a mask.  Bits
+ * follow from the call's sizes and from the visible counts of the rows that
+ * share a tile.
+ */
+int wf_cache_attend_window(wf_cache_t cache, int32_t precision, const wf_rows *q, const wf_rows *out, int32_t B,
+                           int32_t n, int32_t q_heads, const int32_t *table, int32_t table_pages,
+                           const int32_t *visible, int32_t window, int32_t sinks, int32_t max_visible, float scale,
+                           hipStream_t stream);
+
+/*
+ * The same attention for a batch that shares a prefix, which lies in the cache
+ * once: row i of sequence b sees the prefix's tokens j < prefix_visible[b][i]
+ * and its sequence's own j < visible[b][i], under one softmax.  The sequence's
+ * own tokens begin at the start of its first page.  Where it pays, the prefix is
+ * read and multiplied once for the rows of all sequences.
+ *   prefix_table    [prefix_pages] DEVICE int32 page numbers
+ *   prefix_visible  [B][n] DEVICE int32: 0 for a row that takes no part in the
+ *                   prefix (or is not in use, with visible 0)
+ *   max_prefix      no row sees more of the prefix; a row that does is cut there,
+ *                   and the next wf_cache_sync returns WF_E_CAPACITY
+ * The rest, the errors among it, as for wf_cache_attend without a mask;
+ * max_prefix and max_visible are together at most 2^31 - 129.  Bits follow from
+ * the call's sizes and from the counts of the rows that share a tile, which may
+ * be of several sequences.
+ */
+int wf_cache_attend_shared(wf_cache_t cache, int32_t precision, const wf_rows *q, const wf_rows *out, int32_t B,
+                           int32_t n, int32_t q_heads, const int32_t *prefix_table, int32_t prefix_pages,
+                           const int32_t *prefix_visible, int32_t max_prefix, const int32_t *table,
+                           int32_t table_pages, const int32_t *visible, int32_t max_visible, float scale,
+                           hipStream_t stream);
+
 /* Wait for `stream` and report an error that the cache's kernels recorded
  * (see the calls above), on this stream or another.  Clears it; what is
  * recorded while it does so is reported then or by the next one. */

@@ -54,6 +54,14 @@ typedef unsigned u2 __attribute__((ext_vector_type(2)));
 // read-only for the whole launch, at addresses that a wave shares: scalar loads
 typedef const int __attribute__((address_space(4))) * SharedInts;
 
+// Forms of the kernel.  Rows see a prefix of their sequence (kAtMask: what a mask
+// leaves of it); two runs of tokens, the first of its own table (kAtRuns); or the
+// rows of all sequences a first run together, as workgroups before those of each
+// sequence's own tokens, and a kernel of its own joins both (kAtStack).
+enum AtMode { kAtPlain, kAtMask, kAtRuns, kAtStack };
+template <int MODE>
+using AtArgs = std::conditional_t<MODE == kAtPlain || MODE == kAtMask, AttendArgs, AttendRunsArgs>;
+
 constexpr int kAtMaxSplits = 256;
 constexpr int kAtJoin = 256;        // threads of the kernel that joins the splits
 // Waves of a workgroup.  (16 instead of 8: 8.4 against 7.4 us for a token over
@@ -311,21 +319,39 @@ __device__ __forceinline__ int by_length(const AttendArgs& a, int place, int ahe
 
 // One workgroup: 16 NT rows of a sequence's key head, and a share of its
 // tokens.
-template <int DP, class T, int NT, bool MASK>
-__global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, NT>)) void k_attend(AttendArgs a) {
+template <int DP, class T, int NT, int MODE>
+__global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, NT>)) void k_attend(AtArgs<MODE> a) {
+    constexpr bool MASK = MODE == kAtMask, RUNS = MODE == kAtRuns, STACK = MODE == kAtStack;
     constexpr int NW = kAtWaves<DP, T, NT>, NQ = AtParts<T>::kQ, NP = AtParts<T>::kP, NK = DP / 32, ND = DP / 16;
     using L = KvLayout<DP>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
-    const int rows = a.n * a.group, nrt = (rows + 16 * NT - 1) / (16 * NT);
-    const int group = a.splits_(blockIdx.x), split = blockIdx.x - group * a.splits;
-    const int bh = a.tiles_(group), place = group - bh * nrt;
+    // what the workgroup takes: a sequence's own tokens, or all sequences' rows
+    // over the prefix as if they were one's
+    int block = blockIdx.x, n = a.n, splits = a.splits, max_visible = a.max_visible, table_pages = a.table_pages;
+    const int *visible = a.visible, *of_table = a.table;
+    KvDiv splits_ = a.splits_, tiles_ = a.tiles_;
+    bool stacked = false;
+    if constexpr (STACK) {
+        stacked = block < a.stack_blocks;
+        if (stacked) {
+            n = a.B * a.n;
+            splits = a.stack_splits; splits_ = a.stack_splits_; tiles_ = a.stack_tiles_;
+            max_visible = a.max_first; table_pages = a.first_pages;
+            visible = a.first_visible; of_table = a.first_table;
+        } else {
+            block -= a.stack_blocks;
+        }
+    }
+    const int rows = n * a.group, nrt = (rows + 16 * NT - 1) / (16 * NT);
+    const int group = splits_(block), split = block - group * splits;
+    const int bh = tiles_(group), place = group - bh * nrt;
     const int rt = nrt - 1 - place;                    // under a causal order the last rows see most: first
     int b = a.heads_(bh);
     const int head = bh - b * a.c.heads;
-    if constexpr (NT == 1)
+    if constexpr (NT == 1 && (MODE == kAtPlain || MODE == kAtMask))
         if (a.ahead) b = by_length(a, b, a.ahead);
 
-    const SharedInts table = (SharedInts)(a.table + (size_t)b * a.table_pages);
+    const SharedInts table = (SharedInts)(of_table + (size_t)b * table_pages);
     const int in_page = a.c.page_shift - 5;
     const uint8_t* pool = a.c.pool + (size_t)head * a.c.head_bytes();
     const size_t page_bytes = a.c.page_bytes();
@@ -333,9 +359,11 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     // What the rows see, their queries, and the page that the wave begins with
     // if a row sees all it may: in flight together, since each waits as long as
     // a short call's whole arithmetic takes.
-    const int expect = (a.splits_((a.max_visible + kKvTile - 1) / kKvTile + a.splits - 1) * split + wave) >> in_page;
-    const int expected = a.max_visible ? table[min(expect, a.table_pages - 1)] : 0;
-    int see[NT], most = 0, least = a.max_visible;
+    const int expect = RUNS ? -1 : (int)(splits_((max_visible + kKvTile - 1) / kKvTile + splits - 1) * split + wave) >> in_page;
+    const int expected = !RUNS && max_visible ? table[min(expect, table_pages - 1)] : 0;
+    int see[NT], most = 0, least = max_visible;
+    int see_first[NT];                                 // kAtRuns: tokens of the first run,
+    unsigned from[NT];                                 // and the first token of the second
     T raw[NT][NK][8];
     const uint8_t* mask[NT];
 #pragma unroll
@@ -343,27 +371,75 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
         const int row = rt * 16 * NT + t * 16 + col;
         const bool on = row < rows;                    // a column past the last row repeats the first
         const int i = on ? a.group_(row) : 0, h = (head - i) * a.group + (on ? row : 0);
-        see[t] = a.visible[(size_t)b * a.n + i];
-        mask[t] = MASK ? a.mask + b * a.mb + i * a.mr : nullptr;
-        const T* p = (const T*)a.q.p + b * a.q.sb + i * a.q.sr + h * a.q.sh;
+        see[t] = visible[(size_t)b * n + i];
+        if constexpr (RUNS) see_first[t] = a.window ? 0 : a.first_visible[(size_t)b * n + i];
+        mask[t] = nullptr;
+        if constexpr (MASK) mask[t] = a.mask + b * a.mb + i * a.mr;
+        const T* p = (const T*)a.q.p + h * a.q.sh;
+        if constexpr (STACK) {
+            const int of = stacked ? (int)a.n_(i) : b;
+            p += of * a.q.sb + (stacked ? i - of * a.n : i) * a.q.sr;
+        } else {
+            p += b * a.q.sb + i * a.q.sr;
+        }
 #pragma unroll
         for (int kk = 0; kk < NK; ++kk) __builtin_memcpy(raw[t][kk], p + min(DP / 4 * g + 8 * kk, a.c.dim - 8), sizeof raw[t][kk]);
     }
     __builtin_amdgcn_sched_barrier(0);
+    // kAtRuns: the least and most tokens of the first run, and the least and
+    // most of the second's first tokens, that a row sees
+    int least_first = 0, most_first = 0, low = 0, high = 0;
+    if constexpr (RUNS) {
+        least_first = a.max_first;
+        low = max_visible;
+    }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const bool on = rt * 16 * NT + t * 16 + col < rows;
-        if (on && see[t] > a.max_visible) atomicOr(a.c.err, kErrKvRange);
-        see[t] = on ? max(0, min(see[t], a.max_visible)) : 0;
+        if (on && see[t] > max_visible) atomicOr(a.c.err, kErrKvRange);
+        if constexpr (STACK)                           // no workgroups look at the rows' own tokens
+            if (!a.splits && on && a.visible[a.group_(rt * 16 * NT + t * 16 + col)] > 0) atomicOr(a.c.err, kErrKvRange);
+        see[t] = on ? max(0, min(see[t], max_visible)) : 0;
         most = max(most, see[t]);
         if (on) least = min(least, see[t]);
+        if constexpr (RUNS) {
+            from[t] = 0;
+            if (a.window) {
+                // the first tokens are a run of their own where the window does
+                // not reach them
+                const int start = see[t] - a.window;
+                if (start > a.sinks) {
+                    from[t] = start;
+                    see_first[t] = a.sinks;
+                }
+            } else {
+                if (on && see_first[t] > a.max_first) atomicOr(a.c.err, kErrKvRange);
+                see_first[t] = on ? max(0, min(see_first[t], a.max_first)) : 0;
+            }
+            most_first = max(most_first, see_first[t]);
+            if (on) least_first = min(least_first, see_first[t]);
+            if (see[t]) low = min(low, (int)from[t]);
+            high = max(high, (int)from[t]);
+        }
     }
     most = __builtin_amdgcn_readfirstlane(lanes16(most, [](int x, int y) { return max(x, y); }));
     least = __builtin_amdgcn_readfirstlane(lanes16(least, [](int x, int y) { return min(x, y); }));
 
     // the tiles of this split, dealt to the waves in turn
-    const int tiles = (most + kKvTile - 1) / kKvTile;
-    const int share = a.splits_(tiles + a.splits - 1);
+    int tiles = (most + kKvTile - 1) / kKvTile;
+    int first_tiles = 0, skip = 0;                     // tile first_tiles + x is the second run's tile skip + x
+    SharedInts first_table = table;
+    if constexpr (RUNS) {
+        if (!a.window) first_table = (SharedInts)a.first_table;
+        most_first = __builtin_amdgcn_readfirstlane(lanes16(most_first, [](int x, int y) { return max(x, y); }));
+        least_first = __builtin_amdgcn_readfirstlane(lanes16(least_first, [](int x, int y) { return min(x, y); }));
+        low = __builtin_amdgcn_readfirstlane(lanes16(low, [](int x, int y) { return min(x, y); }));
+        high = __builtin_amdgcn_readfirstlane(lanes16(high, [](int x, int y) { return max(x, y); }));
+        first_tiles = (most_first + kKvTile - 1) / kKvTile;
+        skip = min(low / kKvTile, tiles);
+        tiles += first_tiles - skip;
+    }
+    const int share = splits_(tiles + splits - 1);
     const int t0 = split * share, t1 = min(tiles, t0 + share);
 
     b8 q[NT][NK][NQ];
@@ -418,9 +494,14 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
             AtKeys<DP> keys;
             AtValues<DP> values;
             u2 allow[NT];                  // the mask's bytes of the lane's tokens
-            auto page_of = [&](int tile) { return table[min(tile, t1 - 1) >> in_page]; };
+            // where a tile lies in its run
+            auto place_of = [&](int tile) { return RUNS && tile >= first_tiles ? tile - first_tiles + skip : tile; };
+            auto page_of = [&](int tile) {
+                const int u = min(tile, t1 - 1);
+                return RUNS && u < first_tiles ? first_table[place_of(u) >> in_page] : table[place_of(u) >> in_page];
+            };
             auto record_of = [&](int tile, int page) {
-                return pool + (size_t)page * page_bytes + (size_t)(min(tile, t1 - 1) & ((1 << in_page) - 1)) * L::kRecord;
+                return pool + (size_t)page * page_bytes + (size_t)(place_of(min(tile, t1 - 1)) & ((1 << in_page) - 1)) * L::kRecord;
             };
             auto load_mask = [&](int tile) {
                 const int at = min(tile, t1 - 1) * kKvTile + 8 * g;
@@ -462,19 +543,24 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                 add_scores<DP, NT, NQ, 0>(keys, q, s);
                 add_scores<DP, NT, NQ, 1>(keys, q, s);
                 load_keys(keys, record, lane);
-                const int at = tile * kKvTile + 8 * g;         // the lane's first token
-                const bool edge = MASK || !there || (tile + 1) * kKvTile > least;   // some row may not see all of it
+                const bool in_first = RUNS && tile < first_tiles;
+                const int spot = place_of(tile), at = spot * kKvTile + 8 * g;       // the lane's first token
+                bool edge = MASK || !there;                    // some row may not see all of it
+                if constexpr (RUNS) edge |= in_first ? (spot + 1) * kKvTile > least_first : (spot + 1) * kKvTile > least || spot * kKvTile < high;
+                else edge |= (tile + 1) * kKvTile > least;
                 unsigned sees[NT];                     // the lane's tokens that its row sees
 #pragma unroll
                 for (int t = 0; t < NT; ++t) sees[t] = 0xff;
                 if (edge) {
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
-                        const int left = there ? see[t] - at : 0;
+                        const int left = there ? (in_first ? see_first[t] : see[t]) - at : 0;
+                        const int before = RUNS && !in_first ? (int)from[t] - at : 0;
                         sees[t] = 0;
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
                             bool on = e < left;
+                            if constexpr (RUNS) on = on && e >= before;
                             if constexpr (MASK) on = on && (allow[t][e / 4] >> 8 * (e % 4) & 0xff);
                             sees[t] |= (unsigned)on << e;
                             s[t][e / 4][e % 4] = on ? s[t][e / 4][e % 4] : -INFINITY;
@@ -486,8 +572,12 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                 all |= !edge;
                 if (edge) {
                     // past the last token that any row sees, a page holds anything
-                    const int n = max(0, min(8, there ? most - at : 0));
-                    const uint64_t in = n == 8 ? ~0ull : (1ull << 8 * n) - 1;
+                    const int n = max(0, min(8, there ? (in_first ? most_first : most) - at : 0));
+                    uint64_t in = n == 8 ? ~0ull : (1ull << 8 * n) - 1;
+                    if constexpr (RUNS) {              // and before the first
+                        const int m = max(0, min(8, in_first ? 0 : low - at));
+                        in &= m == 8 ? 0ull : ~0ull << 8 * m;
+                    }
                     values.power[0] = (values.power[0] & (unsigned)in) | (0x7f7f7f7fu & ~(unsigned)in);
                     values.power[1] = (values.power[1] & (unsigned)(in >> 32)) | (0x7f7f7f7fu & ~(unsigned)(in >> 32));
                 }
@@ -568,7 +658,10 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     __shared__ __attribute__((aligned(16))) float lds[NW * 16 * kPitch];
     __shared__ float sm[NW][16], sl[NW][16], top[16];
     const int row0 = rt * 16 * NT, here = min(16 * NT, rows - row0);
-    const size_t part = (((size_t)(b * a.c.heads + head) * nrt + place) * a.splits + split) * 16 * NT;
+    size_t part = (((size_t)(b * a.c.heads + head) * nrt + place) * splits + split) * 16 * NT;
+    if constexpr (STACK)
+        if (!stacked) part += a.own_part;
+    const bool whole = !STACK && splits == 1;          // nothing is left to join
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         if (t) __syncthreads();
@@ -597,7 +690,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                 by[w] = at_weight(sm[w][c], sl[w][c], most);
                 sum += by[w] * sl[w][c];
             }
-            const float scale = a.splits > 1 ? 1.0f : at_scale(most, sum);
+            const float scale = whole ? at_scale(most, sum) : 1.0f;
 #pragma unroll
             for (int w = 0; w < NW; ++w) sm[w][c] = by[w] * scale;
             top[c] = most;
@@ -613,7 +706,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                 __builtin_memcpy(&y, __builtin_assume_aligned(&lds[(w * 16 + c) * kPitch + d], 16), sizeof y);
                 v += sm[w][c] * y;
             }
-            if (a.splits == 1) {
+            if (whole) {
                 if (d < a.c.dim) write_row<T>(a, b, head, row0 + t * 16 + c, d, v);
             } else {
                 const size_t at = part + t * 16 + c;
@@ -632,8 +725,8 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
 // weights while the partial results are on their way.  Bound by its chain of
 // launch, load and two exchanges: 3.9 us for 225 rows in 17 splits, 4.7 for 32
 // rows in 32.
-template <int DP, class T, int NT>
-__global__ __launch_bounds__(kAtJoin) void k_attend_join(AttendArgs a) {
+template <int DP, class T, int NT, int MODE>
+__global__ __launch_bounds__(kAtJoin) void k_attend_join(AtArgs<MODE> a) {
     constexpr int W = DP / 8, G = kAtJoin / W, K = kAtMaxSplits / 64, Y = 4;
     __shared__ float weight[kAtMaxSplits];
     __shared__ __attribute__((aligned(16))) float so[kAtJoin / 64][DP];
@@ -641,17 +734,31 @@ __global__ __launch_bounds__(kAtJoin) void k_attend_join(AttendArgs a) {
     const unsigned rows = a.n * a.group, row = blockIdx.x, bh = blockIdx.y;
     const int g = threadIdx.x / W, d = threadIdx.x % W * 8, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const unsigned nrt = (rows + tile_rows - 1) / tile_rows;
-    const size_t first = ((size_t)bh * nrt + (nrt - 1 - row / tile_rows)) * a.splits * tile_rows + row % tile_rows;
-    const float* po = a.part_o + first * DP + d;
+    const int b = a.heads_(bh);
+    size_t first = ((size_t)bh * nrt + (nrt - 1 - row / tile_rows)) * a.splits * tile_rows + row % tile_rows, stacked = 0;
+    int splits = a.splits;
+    if constexpr (MODE == kAtStack) {
+        const unsigned all = a.B * rows, at = b * rows + row, tiles = (all + tile_rows - 1) / tile_rows;
+        stacked = ((size_t)(bh - b * a.c.heads) * tiles + (tiles - 1 - at / tile_rows)) * a.stack_splits * tile_rows + at % tile_rows;
+        first += a.own_part;
+        splits += a.stack_splits;
+    }
+    // the row of a split's partial result
+    auto part = [&](int s) {
+        s = min(s, splits - 1);
+        if constexpr (MODE == kAtStack) return s < a.stack_splits ? stacked + (size_t)s * tile_rows : first + (size_t)(s - a.stack_splits) * tile_rows;
+        else return first + (size_t)s * tile_rows;
+    };
+    const float* po = a.part_o + d;
     f2 z[K];
     if (wave == 0)
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            __builtin_memcpy(&z[k], __builtin_assume_aligned(a.part_ml + (first + (size_t)min(k * 64 + lane, a.splits - 1) * tile_rows) * 2, 8), 8);
+            __builtin_memcpy(&z[k], __builtin_assume_aligned(a.part_ml + part(k * 64 + lane) * 2, 8), 8);
     f8 y[Y];
 #pragma unroll
     for (int j = 0; j < Y; ++j)
-        __builtin_memcpy(&y[j], __builtin_assume_aligned(po + (size_t)min(g + j * G, a.splits - 1) * tile_rows * DP, 16), 32);
+        __builtin_memcpy(&y[j], __builtin_assume_aligned(po + part(g + j * G) * DP, 16), 32);
     __builtin_amdgcn_sched_barrier(0);
     if (wave == 0) {
         float most = -INFINITY, sum = 0.0f;
@@ -660,7 +767,7 @@ __global__ __launch_bounds__(kAtJoin) void k_attend_join(AttendArgs a) {
         most = lanes64(most, [](float x, float y) { return fmaxf(x, y); });
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            z[k][0] = k * 64 + lane < a.splits ? at_weight(z[k][0], z[k][1], most) : 0.0f;
+            z[k][0] = k * 64 + lane < splits ? at_weight(z[k][0], z[k][1], most) : 0.0f;
             sum += z[k][0] * z[k][1];
         }
         sum = lanes64(sum, [](float x, float y) { return x + y; });
@@ -670,17 +777,17 @@ __global__ __launch_bounds__(kAtJoin) void k_attend_join(AttendArgs a) {
     }
     __syncthreads();
     f8 v = {};
-    for (int s = g; s < a.splits; s += Y * G) {
+    for (int s = g; s < splits; s += Y * G) {
         float by[Y];
 #pragma unroll
         for (int j = 0; j < Y; ++j) by[j] = weight[min(s + j * G, kAtMaxSplits - 1)];
 #pragma unroll
         for (int j = 0; j < Y; ++j)
-            if (s + j * G < a.splits) v += by[j] * y[j];
-        if (s + Y * G < a.splits)
+            if (s + j * G < splits) v += by[j] * y[j];
+        if (s + Y * G < splits)
 #pragma unroll
             for (int j = 0; j < Y; ++j)
-                __builtin_memcpy(&y[j], __builtin_assume_aligned(po + (size_t)min(s + (Y + j) * G, a.splits - 1) * tile_rows * DP, 16), 32);
+                __builtin_memcpy(&y[j], __builtin_assume_aligned(po + part(s + (Y + j) * G) * DP, 16), 32);
     }
     // the groups of a wave, then the waves
 #pragma unroll
@@ -696,7 +803,6 @@ __global__ __launch_bounds__(kAtJoin) void k_attend_join(AttendArgs a) {
         __builtin_memcpy(&z, __builtin_assume_aligned(&so[w][d], 16), 32);
         v += z;
     }
-    const int b = a.heads_(bh);
     write_row<T>(a, b, bh - b * a.c.heads, row, d, v);
 }
 
@@ -718,7 +824,8 @@ static int row_tiles(const AttendArgs& a, int precision) {
     return rows > 16 && tiles * a.c.dp >= kAtManyRows && a.c.dp * (precision == WF_BF16 ? 2 : 4) <= 256 ? 2 : 1;
 }
 
-long long attend_plan(AttendArgs& a, int precision) {
+// How the tiles of a workgroup's rows are split.  Returns the threads of the launch.
+static long long split_plan(AttendArgs& a, int precision, long long tiles) {
     const int bytes = a.c.dp * (precision == WF_BF16 ? 2 : 4), nt = row_tiles(a, precision), rows = a.n * a.group;
     const int waves = nt == 1 && bytes < 1024 ? 8 : 4;
     const long long groups = (long long)a.B * a.c.heads * ((rows + 16 * nt - 1) / (16 * nt));
@@ -727,7 +834,6 @@ long long attend_plan(AttendArgs& a, int precision) {
     // tiles each, two and one: a token over 1001 (8 heads of 128, bf16) 7.3, 7.4,
     // 8.3, 7.4, over 2047 11.0, 10.2, 8.5, 7.8, over 8192 33, 10.6, 9.1, 8.7; 45
     // fp32 rows over 1024 7.2, 7.2, 8.5, 7.8, over 4096 16.9, 10.7, 9.0, 8.5.
-    const long long tiles = ((long long)a.max_visible + kKvTile - 1) / kKvTile;
     const long long by_len = tiles <= 4 * waves ? 1 : (tiles + waves - 1) / waves;
     long long s = kAtTarget / groups;
     // Long calls (8192 tokens) that would leave many compute units idle take two
@@ -751,6 +857,15 @@ long long attend_plan(AttendArgs& a, int precision) {
     a.tiles_.by((unsigned)((rows + 16 * nt - 1) / (16 * nt)));
     a.heads_.by(a.c.heads);
     a.group_.by(a.group);
+    return groups * a.splits * waves * 64;
+}
+
+static long long tiles_of(long long tokens) { return (tokens + kKvTile - 1) / kKvTile; }
+
+long long attend_plan(AttendArgs& a, int precision) {
+    const int bytes = a.c.dp * (precision == WF_BF16 ? 2 : 4), nt = row_tiles(a, precision), rows = a.n * a.group;
+    const long long groups = (long long)a.B * a.c.heads * ((rows + 16 * nt - 1) / (16 * nt));
+    const long long threads = split_plan(a, precision, tiles_of(a.max_visible));
     // A token each of sequences that may be of unequal lengths, and two
     // workgroups on most compute units.  With more of them the units take the
     // next as they finish: in the order given and longest first, 128 sequences
@@ -758,44 +873,118 @@ long long attend_plan(AttendArgs& a, int precision) {
     // to 8192 226 / 228, of 8192 each 395 / 406.
     const bool two = groups > kAtTarget && groups <= 2 * kAtTarget && bytes <= 256 && a.splits == 1;
     a.ahead = nt == 1 && rows <= 16 && a.B > 1 && a.B <= kAtBatch && two ? (int)(kAtTarget / a.c.heads) : 0;
-    return groups * a.splits * waves * 64;
+    return threads;
 }
 
-template <int DP, class T, int NT>
-static void join(const AttendArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL((k_attend_join<DP, T, NT>), dim3(a.n * a.group, a.B * a.c.heads), dim3(kAtJoin), 0, st, a);
+// A window's rows read its tokens, those that the other rows of their tile are
+// ahead by under a causal order, and the first tokens.
+long long attend_window_plan(AttendRunsArgs& a, int precision) {
+    const int rows = 16 * row_tiles(a, precision), apart = (rows + a.group - 1) / a.group, ahead = (apart < a.n ? apart : a.n) - 1;
+    const long long all = tiles_of(a.max_visible), some = tiles_of(a.sinks) + tiles_of((long long)a.window + ahead) + 1;
+    return split_plan(a, precision, some < all ? some : all);
 }
 
-template <int DP, class T, int NT>
-static void launch_nt(const AttendArgs& a, hipStream_t st) {
+// The rows of all sequences over the prefix and each one's over its own tokens in
+// one launch.  False where their partial results do not fit the workspace.
+static bool stack_plan(AttendRunsArgs& a, int precision, int nt) {
+    const int waves = nt == 1 && a.c.dp * (precision == WF_BF16 ? 2 : 4) < 1024 ? 8 : 4;
+    const long long rows = (long long)a.n * a.group, tile = 16 * nt;
+    const long long shared = a.c.heads * ((a.B * rows + tile - 1) / tile), own = a.max_visible ? a.B * a.c.heads * ((rows + tile - 1) / tile) : 0;
+    const long long shared_tiles = tiles_of(a.max_first), own_tiles = tiles_of(a.max_visible);
+    const long long room = (long long)attend_work_rows(a.c.dp) / tile;
+    if (shared + own > room) return false;
+    // Both parts are split into shares of as many tiles, so many that the chip is
+    // filled, down to a tile a wave: there is a join in any case.
+    long long share = (shared * shared_tiles + own * own_tiles + kAtTarget * 2 - 1) / (kAtTarget * 2);
+    share = share < waves ? waves : share;
+    long long s, o;
+    for (;; share += (share + 7) / 8) {
+        s = (shared_tiles + share - 1) / share;
+        o = own ? (own_tiles + share - 1) / share : 0;
+        if (s + o <= kAtMaxSplits && shared * s + own * o <= room) break;
+    }
+    a.stack_splits = (int)s; a.splits = (int)o;
+    a.stack_splits_.by((unsigned)s); a.splits_.by(o ? (unsigned)o : 1u);
+    a.stack_tiles_.by((unsigned)((a.B * rows + tile - 1) / tile)); a.tiles_.by((unsigned)((rows + tile - 1) / tile));
+    a.heads_.by(a.c.heads); a.group_.by(a.group); a.n_.by(a.n);
+    a.stack_blocks = (int)(shared * s);
+    a.own_part = shared * s * tile;
+    return true;
+}
+
+static int stack_row_tiles(const AttendRunsArgs& a, int precision) { return a.c.dp * (precision == WF_BF16 ? 2 : 4) <= 256 ? 2 : 1; }
+
+long long attend_shared_plan(AttendRunsArgs& a, int precision, int* together) {
+    const int nt = stack_row_tiles(a, precision);
+    const long long rows = (long long)a.n * a.group, tile = 16 * nt, first = tiles_of(a.max_first), own = tiles_of(a.max_visible);
+    // Tiles that workgroups take, with the rows together over the prefix and apart.
+    const long long apart = a.B * ((rows + tile - 1) / tile) * (first + own);
+    const long long joint = (a.B * rows + tile - 1) / tile * first + a.B * ((rows + tile - 1) / tile) * own;
+    *together = 0;
+    if (a.B > 1 && first && 5 * joint < 4 * apart && a.B * rows < 1LL << 24) {
+        AttendRunsArgs x = a;
+        for (x.B = a.B; x.B > 1 && !stack_plan(x, precision, nt);) x.B = (x.B + 1) / 2 == x.B ? 1 : (x.B + 1) / 2;
+        if (x.B > 1) *together = x.B;
+    }
+    if (*together) return 0;
+    return split_plan(a, precision, first + own);
+}
+
+// The kernel of a form and, where its calls are split, the join.
+template <int DP, class T, int NT, int MODE>
+static void launch_form(const AtArgs<MODE>& a, hipStream_t st) {
     const int rows = a.n * a.group;
-    const long long groups = (long long)a.B * a.c.heads * ((rows + 16 * NT - 1) / (16 * NT));
-    constexpr int kThreads = 64 * kAtWaves<DP, T, NT>;
-    const dim3 grid((unsigned)(groups * a.splits));
-    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, a); };
-    if (a.mask) launch(k_attend<DP, T, NT, true>);
-    else launch(k_attend<DP, T, NT, false>);
-    if (a.splits > 1) join<DP, T, NT>(a, st);
+    long long groups = (long long)a.B * a.c.heads * ((rows + 16 * NT - 1) / (16 * NT)) * a.splits;
+    if constexpr (MODE == kAtStack) groups += a.stack_blocks;
+    hipLaunchKernelGGL((k_attend<DP, T, NT, MODE>), dim3((unsigned)groups), dim3(64 * kAtWaves<DP, T, NT>), 0, st, a);
+    if (MODE == kAtStack || a.splits > 1)
+        hipLaunchKernelGGL((k_attend_join<DP, T, NT, MODE == kAtMask ? kAtPlain : MODE>), dim3(a.n * a.group, a.B * a.c.heads), dim3(kAtJoin), 0, st, a);
 }
 
-template <int DP, class T>
-static void launch_dp(const AttendArgs& a, int nt, hipStream_t st) {
+template <int DP, class T, int MODE>
+static void launch_nt(const AtArgs<MODE>& a, int nt, hipStream_t st) {
     if constexpr (kAtTwoTiles<DP, T>)
-        if (nt == 2) return launch_nt<DP, T, 2>(a, st);
-    launch_nt<DP, T, 1>(a, st);
+        if (nt == 2) return launch_form<DP, T, 2, MODE>(a, st);
+    launch_form<DP, T, 1, MODE>(a, st);
 }
 
-template <class T>
-static void launch_precision(const AttendArgs& a, int nt, hipStream_t st) {
-    if (a.c.dp == 64) launch_dp<64, T>(a, nt, st);
-    else if (a.c.dp == 128) launch_dp<128, T>(a, nt, st);
-    else launch_dp<256, T>(a, nt, st);
+template <class T, int MODE>
+static void launch_dp(const AtArgs<MODE>& a, int nt, hipStream_t st) {
+    if (a.c.dp == 64) launch_nt<64, T, MODE>(a, nt, st);
+    else if (a.c.dp == 128) launch_nt<128, T, MODE>(a, nt, st);
+    else launch_nt<256, T, MODE>(a, nt, st);
+}
+
+template <int MODE>
+static void launch(const AtArgs<MODE>& a, int precision, int nt, hipStream_t st) {
+    if (precision == WF_BF16) launch_dp<__bf16, MODE>(a, nt, st);
+    else launch_dp<float, MODE>(a, nt, st);
 }
 
 void launch_attend(const AttendArgs& a, int precision, hipStream_t st) {
     const int nt = row_tiles(a, precision);
-    if (precision == WF_BF16) launch_precision<__bf16>(a, nt, st);
-    else launch_precision<float>(a, nt, st);
+    if (a.mask) launch<kAtMask>(a, precision, nt, st);
+    else launch<kAtPlain>(a, precision, nt, st);
+}
+
+void launch_attend_window(const AttendRunsArgs& a, int precision, hipStream_t st) { launch<kAtRuns>(a, precision, row_tiles(a, precision), st); }
+
+void launch_attend_shared(const AttendRunsArgs& a, int precision, int together, hipStream_t st) {
+    if (!together) return launch<kAtRuns>(a, precision, row_tiles(a, precision), st);
+    // sequences in turn, since the launches share the workspace
+    const int nt = stack_row_tiles(a, precision);
+    const size_t item = precision == WF_BF16 ? 2 : 4;
+    for (int b = 0; b < a.B; b += together) {
+        AttendRunsArgs x = a;
+        x.B = together < a.B - b ? together : a.B - b;
+        x.q.p = (char*)a.q.p + b * a.q.sb * (long long)item;
+        x.o.p = (char*)a.o.p + b * a.o.sb * (long long)item;
+        x.table += (size_t)b * a.table_pages;
+        x.visible += (size_t)b * a.n;
+        x.first_visible += (size_t)b * a.n;
+        stack_plan(x, precision, nt);
+        launch<kAtStack>(x, precision, nt, st);
+    }
 }
 
 }  // namespace wf

@@ -168,10 +168,29 @@ struct AttendArgs {
     float *part_o, *part_ml;         // partial results: channels, and (maximum, sum)
 };
 
+// What the kernels of the other forms need beside: a first run of tokens before
+// the sequence's own.
+struct AttendRunsArgs : AttendArgs {
+    // a prefix that lies in the cache once
+    const int *first_table, *first_visible;
+    int first_pages, max_first;
+    int window, sinks;               // window > 0: the first run is the sequence's first tokens
+    // rows of all sequences together over the prefix, as workgroups before the others
+    int stack_blocks, stack_splits;
+    KvDiv stack_splits_, stack_tiles_, n_;
+    long long own_part;              // the first row of the others' partial results
+};
+
 void launch_kv_write(const KvCache&, int precision, const KvRows& k, const KvRows& v, const KvTokens&, hipStream_t);
 void launch_kv_read(const KvCache&, int precision, const KvRows& k, const KvRows& v, const KvTokens&, hipStream_t);
 // The splits of a call.  Returns the threads of its launch.
 long long attend_plan(AttendArgs&, int precision);
 void launch_attend(const AttendArgs&, int precision, hipStream_t);
+long long attend_window_plan(AttendRunsArgs&, int precision);
+void launch_attend_window(const AttendRunsArgs&, int precision, hipStream_t);
+// Sequences that a launch takes together (0: every sequence for itself, in one
+// launch), and the threads of the largest.
+long long attend_shared_plan(AttendRunsArgs&, int precision, int* together);
+void launch_attend_shared(const AttendRunsArgs&, int precision, int together, hipStream_t);
 
 }  // namespace wf

@@ -288,6 +288,36 @@ static int kv_tokens(const Cache* c, int precision, int B, int n, const int32_t*
     return WF_OK;
 }
 
+// What the attention calls have in common: their checks, and the arguments but
+// for the split.
+static int kv_attend(const Cache* c, int precision, const wf_rows* q, const wf_rows* out, int B, int n, int q_heads, const int32_t* table,
+                     int table_pages, const int32_t* visible, int max_visible, float scale, AttendArgs* to) {
+    AttendArgs& a = *to;
+    if (!c) return fail(WF_E_INVALID, "cache is NULL");
+    if (precision != WF_FP32 && precision != WF_BF16) return fail(WF_E_INVALID, "unknown precision");
+    if (B < 0 || n < 0 || table_pages < 0) return fail(WF_E_INVALID, "B, n and table_pages must not be negative");
+    if (q_heads < 1 || q_heads % c->c.heads) return fail(WF_E_INVALID, "q_heads must be a positive multiple of the cache's heads");
+    if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(WF_E_INVALID, "scale must be positive and finite");
+    if (max_visible < 0 || max_visible > (long long)table_pages << c->c.page_shift)
+        return fail(WF_E_INVALID, "max_visible must lie in [0, table_pages * page]");
+    // the kernel counts tokens in 32 bits, up to the end of the last one's tile and the next
+    if (max_visible > INT32_MAX - 2 * kKvTile) return fail(WF_E_UNSUPPORTED, "max_visible is beyond 2^31 - 65");
+    if (!B || !n) return WF_OK;
+    if (!visible || (max_visible && !table)) return fail(WF_E_INVALID, "visible or table is NULL");
+    int rc;
+    if ((rc = kv_rows(q, precision, "q", &a.q)) != WF_OK || (rc = kv_rows(out, precision, "out", &a.o)) != WF_OK) return rc;
+    if ((long long)n * (q_heads / c->c.heads) >= 1 << 30 || (long long)B * n * q_heads >= 1LL << 31)
+        return fail(WF_E_UNSUPPORTED, "more than 2^31 query rows in one call");
+    a.c = c->c;
+    a.table = table; a.visible = visible;
+    a.table_pages = table_pages; a.B = B; a.n = n; a.group = q_heads / c->c.heads;
+    a.max_visible = max_visible;
+    a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+    a.part_o = c->work;
+    a.part_ml = c->work + attend_work_rows(c->c.dp) * c->c.dp;
+    return WF_OK;
+}
+
 }  // namespace wf
 
 using namespace wf;
@@ -380,36 +410,68 @@ int wf_cache_attend(wf_cache_t cache, int32_t precision, const wf_rows* q, const
                     int32_t q_heads, const int32_t* table, int32_t table_pages, const int32_t* visible,
                     const uint8_t* mask, const int64_t* mask_stride, int32_t max_visible, float scale, hipStream_t stream) try {
     const Cache* c = reinterpret_cast<Cache*>(cache);
-    if (!c) return fail(WF_E_INVALID, "cache is NULL");
-    if (precision != WF_FP32 && precision != WF_BF16) return fail(WF_E_INVALID, "unknown precision");
-    if (B < 0 || n < 0 || table_pages < 0) return fail(WF_E_INVALID, "B, n and table_pages must not be negative");
-    if (q_heads < 1 || q_heads % c->c.heads) return fail(WF_E_INVALID, "q_heads must be a positive multiple of the cache's heads");
-    if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(WF_E_INVALID, "scale must be positive and finite");
-    if (max_visible < 0 || max_visible > (long long)table_pages << c->c.page_shift)
-        return fail(WF_E_INVALID, "max_visible must lie in [0, table_pages * page]");
-    // the kernel counts tokens in 32 bits, up to the end of the last one's tile and the next
-    if (max_visible > INT32_MAX - 2 * kKvTile) return fail(WF_E_UNSUPPORTED, "max_visible is beyond 2^31 - 65");
     if (mask && !mask_stride) return fail(WF_E_INVALID, "mask_stride is NULL");
-    if (!B || !n) return WF_OK;
-    if (!visible || (max_visible && !table)) return fail(WF_E_INVALID, "visible or table is NULL");
     AttendArgs a{};
-    int rc;
-    if ((rc = kv_rows(q, precision, "q", &a.q)) != WF_OK || (rc = kv_rows(out, precision, "out", &a.o)) != WF_OK) return rc;
-    if ((long long)n * (q_heads / c->c.heads) >= 1 << 30 || (long long)B * n * q_heads >= 1LL << 31)
-        return fail(WF_E_UNSUPPORTED, "more than 2^31 query rows in one call");
-    a.c = c->c;
-    a.table = table; a.visible = visible; a.mask = mask;
+    int rc = kv_attend(c, precision, q, out, B, n, q_heads, table, table_pages, visible, max_visible, scale, &a);
+    if (rc != WF_OK || !B || !n) return rc;
+    a.mask = mask;
     if (mask) { a.mb = mask_stride[0]; a.mr = mask_stride[1]; }
-    a.table_pages = table_pages; a.B = B; a.n = n; a.group = q_heads / c->c.heads;
-    a.max_visible = max_visible;
-    a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     if (attend_plan(a, precision) >= 1LL << 32) return fail(WF_E_UNSUPPORTED, "2^32 or more threads in one call");
-    a.part_o = c->work;
-    a.part_ml = c->work + attend_work_rows(c->c.dp) * c->c.dp;
     const OnDevice on(c->device);
     if (on.error() != hipSuccess) return kv_fail(on.error(), "the cache's device");
     launch_attend(a, precision, stream);
     return kv_launched("wf_cache_attend");
+} catch (...) {
+    return WF_E_NOMEM;
+}
+
+int wf_cache_attend_window(wf_cache_t cache, int32_t precision, const wf_rows* q, const wf_rows* out, int32_t B, int32_t n,
+                           int32_t q_heads, const int32_t* table, int32_t table_pages, const int32_t* visible, int32_t window,
+                           int32_t sinks, int32_t max_visible, float scale, hipStream_t stream) try {
+    const Cache* c = reinterpret_cast<Cache*>(cache);
+    if (window < 1 || sinks < 0) return fail(WF_E_INVALID, "window must be positive and sinks not negative");
+    AttendRunsArgs a{};
+    int rc = kv_attend(c, precision, q, out, B, n, q_heads, table, table_pages, visible, max_visible, scale, &a);
+    if (rc != WF_OK || !B || !n) return rc;
+    a.window = window;
+    a.sinks = sinks < max_visible ? sinks : max_visible;
+    // (where every row sees all that is visible, the window has no part in it)
+    const bool all = (long long)window + sinks >= max_visible;
+    if ((all ? attend_plan(a, precision) : attend_window_plan(a, precision)) >= 1LL << 32)
+        return fail(WF_E_UNSUPPORTED, "2^32 or more threads in one call");
+    const OnDevice on(c->device);
+    if (on.error() != hipSuccess) return kv_fail(on.error(), "the cache's device");
+    if (all) launch_attend(a, precision, stream);
+    else launch_attend_window(a, precision, stream);
+    return kv_launched("wf_cache_attend_window");
+} catch (...) {
+    return WF_E_NOMEM;
+}
+
+int wf_cache_attend_shared(wf_cache_t cache, int32_t precision, const wf_rows* q, const wf_rows* out, int32_t B, int32_t n,
+                           int32_t q_heads, const int32_t* prefix_table, int32_t prefix_pages, const int32_t* prefix_visible,
+                           int32_t max_prefix, const int32_t* table, int32_t table_pages, const int32_t* visible,
+                           int32_t max_visible, float scale, hipStream_t stream) try {
+    const Cache* c = reinterpret_cast<Cache*>(cache);
+    AttendRunsArgs a{};
+    int rc = kv_attend(c, precision, q, out, B, n, q_heads, table, table_pages, visible, max_visible, scale, &a);
+    if (rc != WF_OK) return rc;
+    if (prefix_pages < 0) return fail(WF_E_INVALID, "prefix_pages must not be negative");
+    if (max_prefix < 0 || max_prefix > (long long)prefix_pages << c->c.page_shift)
+        return fail(WF_E_INVALID, "max_prefix must lie in [0, prefix_pages * page]");
+    // tiles of both runs are counted together, in tokens
+    if ((long long)max_prefix + max_visible > INT32_MAX - 4 * kKvTile)
+        return fail(WF_E_UNSUPPORTED, "max_prefix and max_visible are together beyond 2^31 - 129");
+    if (!B || !n) return WF_OK;
+    if (!prefix_visible || (max_prefix && !prefix_table)) return fail(WF_E_INVALID, "prefix_visible or prefix_table is NULL");
+    a.first_table = prefix_table; a.first_visible = prefix_visible;
+    a.first_pages = prefix_pages; a.max_first = max_prefix;
+    int together;
+    if (attend_shared_plan(a, precision, &together) >= 1LL << 32) return fail(WF_E_UNSUPPORTED, "2^32 or more threads in one call");
+    const OnDevice on(c->device);
+    if (on.error() != hipSuccess) return kv_fail(on.error(), "the cache's device");
+    launch_attend_shared(a, precision, together, stream);
+    return kv_launched("wf_cache_attend_shared");
 } catch (...) {
     return WF_E_NOMEM;
 }

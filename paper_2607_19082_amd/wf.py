@@ -26,7 +26,8 @@ DRIVER = {"stream": 0, "graph": 1, "persistent": 2, "dataflow": 3, "resident": 4
 EXPORTS = ["wf_schedule", "wf_validate", "wf_plan", "wf_plan_schedule", "wf_plan_deps", "wf_plan_set_waits", "wf_litmus", "wf_decode",
            "wf_encode", "wf_ec_tables", "wf_mix_tables", "wf_encode_bits", "wf_decode_bits", "wf_plan_trace",
            "wf_measure_floor", "wf_plan_sync", "wf_xform_plan", "wf_hyper_synthesis", "wf_synthesis",
-           "wf_decode_noalloc", "wf_cache_plan", "wf_cache_write", "wf_cache_read", "wf_cache_attend", "wf_cache_sync",
+           "wf_decode_noalloc", "wf_cache_plan", "wf_cache_write", "wf_cache_read", "wf_cache_attend",
+           "wf_cache_attend_window", "wf_cache_attend_shared", "wf_cache_sync",
            "wf_cache_destroy", "wf_head_norm_plan", "wf_head_norm", "wf_head_norm_destroy", "wf_xform_destroy", "wf_plan_destroy", "wf_last_error"]
 
 
@@ -126,6 +127,8 @@ def lib():
         L.wf_cache_write.argtypes = [P, i32, P, P, i32, i32, P, i32, P, P, P]
         L.wf_cache_read.argtypes = [P, i32, P, P, i32, i32, P, i32, P, P, P]
         L.wf_cache_attend.argtypes = [P, i32, P, P, i32, i32, i32, P, i32, P, P, P, i32, ctypes.c_float, P]
+        L.wf_cache_attend_window.argtypes = [P, i32, P, P, i32, i32, i32, P, i32, P, i32, i32, i32, ctypes.c_float, P]
+        L.wf_cache_attend_shared.argtypes = [P, i32, P, P, i32, i32, i32, P, i32, P, i32, P, i32, P, i32, ctypes.c_float, P]
         L.wf_cache_sync.argtypes = [P, P]
         L.wf_head_norm_plan.argtypes = [ctypes.POINTER(HeadNormDesc), ctypes.POINTER(ctypes.c_void_p)]
         L.wf_head_norm.argtypes = [P, i32, P, P, i32, P, P, P, i32, P, i32, i32, P, P, P]
@@ -653,6 +656,62 @@ class Cache(_TokenCalls):
             self._h, precision, q_rows, out_rows, B, n, hq, p_table, pages, self._ints(visible, (B, n), "visible"),
             p_mask, strides, max_visible, self.dim ** -0.5 if scale is None else scale,
             self._stream(stream, q, table, visible, mask, out))
+        if rc:
+            _check(rc)
+        return out
+
+    def _queries(self, q, out, table, max_visible, stream):
+        """What the attention calls check in common: (B, n, query heads, precision,
+        rows of q, out, its rows, table, its pages, max_visible)."""
+        shape, dtype = q.shape, q.dtype
+        if len(shape) != 4:
+            raise ValueError(f"q: expected four dimensions, got {tuple(shape)}")
+        B, n, hq, _ = shape
+        shape, precision = (B, n, hq, self.dim), self._type(dtype)
+        q_rows = self._rows(q, shape, dtype, "q")
+        p_table, pages = self._table(table, B)
+        if max_visible is None:
+            max_visible = pages * self.page
+        if (B | n | hq | pages | max_visible) >> 31:
+            _sizes(B, n, hq, pages, max_visible)
+        if out is None:
+            out, out_rows = self._new(shape, dtype, stream, like=q if q.is_contiguous() else None)
+        else:
+            out_rows = self._rows(out, shape, dtype, "out")
+        return B, n, hq, precision, q_rows, out, out_rows, p_table, pages, max_visible
+
+    def attend_window(self, q, table, visible, window, sinks=0, scale=None, max_visible=None, out=None, stream=None):
+        """As attend, but of the tokens j < visible[b, i] a row sees the last
+        `window` and the first `sinks`.  Pages that no row sees are not read."""
+        B, n, hq, precision, q_rows, out, out_rows, p_table, pages, max_visible = self._queries(q, out, table, max_visible, stream)
+        if (window | sinks) >> 31:
+            _sizes(window, sinks)
+        rc = self._lib.wf_cache_attend_window(
+            self._h, precision, q_rows, out_rows, B, n, hq, p_table, pages, self._ints(visible, (B, n), "visible"), window,
+            sinks, max_visible, self.dim ** -0.5 if scale is None else scale, self._stream(stream, q, table, visible, out))
+        if rc:
+            _check(rc)
+        return out
+
+    def attend_shared(self, q, prefix_table, prefix_visible, table, visible, scale=None, max_prefix=None, max_visible=None,
+                      out=None, stream=None):
+        """As attend, for a batch that shares a prefix: row i of sequence b sees the
+        tokens j < prefix_visible[b, i] of the pages prefix_table (int32
+        [prefix_pages]) and j < visible[b, i] of its own pages, under one softmax.
+        max_prefix bounds prefix_visible (default: all that its table holds)."""
+        B, n, hq, precision, q_rows, out, out_rows, p_table, pages, max_visible = self._queries(q, out, table, max_visible, stream)
+        if len(prefix_table.shape) != 1:
+            raise ValueError(f"prefix_table: expected one dimension, got {tuple(prefix_table.shape)}")
+        prefix_pages = prefix_table.shape[0]
+        if max_prefix is None:
+            max_prefix = prefix_pages * self.page
+        if (prefix_pages | max_prefix) >> 31:
+            _sizes(prefix_pages, max_prefix)
+        rc = self._lib.wf_cache_attend_shared(
+            self._h, precision, q_rows, out_rows, B, n, hq, self._ints(prefix_table, (prefix_pages,), "prefix_table"),
+            prefix_pages, self._ints(prefix_visible, (B, n), "prefix_visible"), max_prefix, p_table, pages,
+            self._ints(visible, (B, n), "visible"), max_visible, self.dim ** -0.5 if scale is None else scale,
+            self._stream(stream, q, prefix_table, prefix_visible, table, visible, out))
         if rc:
             _check(rc)
         return out
