@@ -343,11 +343,25 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
         }
     }
     const int rows = n * a.group, nrt = (rows + 16 * NT - 1) / (16 * NT);
-    const int group = splits_(block), split = block - group * splits;
-    const int bh = tiles_(group), place = group - bh * nrt;
+    int group = splits_(block), split = block - group * splits;
+    const int bh = tiles_(group);
+    int place = group - bh * nrt, b = a.heads_(bh), head = bh - b * a.c.heads;
+    if constexpr (RUNS || STACK)
+        if (a.units_of_die && (RUNS || stacked)) {
+            const int t = block / kXcds, u = a.unit_(t), unit = block % kXcds * a.units_of_die + u, l = t - u * a.unit_workgroups;
+            if constexpr (STACK) {
+                split = l;
+                head = tiles_(unit);
+                place = unit - head * nrt;
+                b = 0;
+            } else {
+                place = splits_(l);
+                split = l - place * splits;
+                head = a.batch_(unit);
+                b = unit - head * a.B;
+            }
+        }
     const int rt = nrt - 1 - place;                    // under a causal order the last rows see most: first
-    int b = a.heads_(bh);
-    const int head = bh - b * a.c.heads;
     if constexpr (NT == 1 && (MODE == kAtPlain || MODE == kAtMask))
         if (a.ahead) b = by_length(a, b, a.ahead);
 
@@ -660,7 +674,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     const int row0 = rt * 16 * NT, here = min(16 * NT, rows - row0);
     size_t part = (((size_t)(b * a.c.heads + head) * nrt + place) * splits + split) * 16 * NT;
     if constexpr (STACK)
-        if (!stacked) part += a.own_part;
+        if (!stacked) part = a.own_part + (((size_t)(b * a.c.heads + head) * nrt + place) * splits + split) * a.own_rows;
     const bool whole = !STACK && splits == 1;          // nothing is left to join
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -725,8 +739,8 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
 // weights while the partial results are on their way.  Bound by its chain of
 // launch, load and two exchanges: 3.9 us for 225 rows in 17 splits, 4.7 for 32
 // rows in 32.
-template <int DP, class T, int NT, int MODE>
-__global__ __launch_bounds__(kAtJoin) void k_attend_join(AtArgs<MODE> a) {
+template <int DP, class T, int NT>
+__global__ __launch_bounds__(kAtJoin) void k_attend_join(AttendArgs a) {
     constexpr int W = DP / 8, G = kAtJoin / W, K = kAtMaxSplits / 64, Y = 4;
     __shared__ float weight[kAtMaxSplits];
     __shared__ __attribute__((aligned(16))) float so[kAtJoin / 64][DP];
@@ -734,31 +748,17 @@ __global__ __launch_bounds__(kAtJoin) void k_attend_join(AtArgs<MODE> a) {
     const unsigned rows = a.n * a.group, row = blockIdx.x, bh = blockIdx.y;
     const int g = threadIdx.x / W, d = threadIdx.x % W * 8, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const unsigned nrt = (rows + tile_rows - 1) / tile_rows;
-    const int b = a.heads_(bh);
-    size_t first = ((size_t)bh * nrt + (nrt - 1 - row / tile_rows)) * a.splits * tile_rows + row % tile_rows, stacked = 0;
-    int splits = a.splits;
-    if constexpr (MODE == kAtStack) {
-        const unsigned all = a.B * rows, at = b * rows + row, tiles = (all + tile_rows - 1) / tile_rows;
-        stacked = ((size_t)(bh - b * a.c.heads) * tiles + (tiles - 1 - at / tile_rows)) * a.stack_splits * tile_rows + at % tile_rows;
-        first += a.own_part;
-        splits += a.stack_splits;
-    }
-    // the row of a split's partial result
-    auto part = [&](int s) {
-        s = min(s, splits - 1);
-        if constexpr (MODE == kAtStack) return s < a.stack_splits ? stacked + (size_t)s * tile_rows : first + (size_t)(s - a.stack_splits) * tile_rows;
-        else return first + (size_t)s * tile_rows;
-    };
-    const float* po = a.part_o + d;
+    const size_t first = ((size_t)bh * nrt + (nrt - 1 - row / tile_rows)) * a.splits * tile_rows + row % tile_rows;
+    const float* po = a.part_o + first * DP + d;
     f2 z[K];
     if (wave == 0)
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            __builtin_memcpy(&z[k], __builtin_assume_aligned(a.part_ml + part(k * 64 + lane) * 2, 8), 8);
+            __builtin_memcpy(&z[k], __builtin_assume_aligned(a.part_ml + (first + (size_t)min(k * 64 + lane, a.splits - 1) * tile_rows) * 2, 8), 8);
     f8 y[Y];
 #pragma unroll
     for (int j = 0; j < Y; ++j)
-        __builtin_memcpy(&y[j], __builtin_assume_aligned(po + part(g + j * G) * DP, 16), 32);
+        __builtin_memcpy(&y[j], __builtin_assume_aligned(po + (size_t)min(g + j * G, a.splits - 1) * tile_rows * DP, 16), 32);
     __builtin_amdgcn_sched_barrier(0);
     if (wave == 0) {
         float most = -INFINITY, sum = 0.0f;
@@ -767,7 +767,7 @@ __global__ __launch_bounds__(kAtJoin) void k_attend_join(AtArgs<MODE> a) {
         most = lanes64(most, [](float x, float y) { return fmaxf(x, y); });
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            z[k][0] = k * 64 + lane < splits ? at_weight(z[k][0], z[k][1], most) : 0.0f;
+            z[k][0] = k * 64 + lane < a.splits ? at_weight(z[k][0], z[k][1], most) : 0.0f;
             sum += z[k][0] * z[k][1];
         }
         sum = lanes64(sum, [](float x, float y) { return x + y; });
@@ -777,17 +777,17 @@ __global__ __launch_bounds__(kAtJoin) void k_attend_join(AtArgs<MODE> a) {
     }
     __syncthreads();
     f8 v = {};
-    for (int s = g; s < splits; s += Y * G) {
+    for (int s = g; s < a.splits; s += Y * G) {
         float by[Y];
 #pragma unroll
         for (int j = 0; j < Y; ++j) by[j] = weight[min(s + j * G, kAtMaxSplits - 1)];
 #pragma unroll
         for (int j = 0; j < Y; ++j)
-            if (s + j * G < splits) v += by[j] * y[j];
-        if (s + Y * G < splits)
+            if (s + j * G < a.splits) v += by[j] * y[j];
+        if (s + Y * G < a.splits)
 #pragma unroll
             for (int j = 0; j < Y; ++j)
-                __builtin_memcpy(&y[j], __builtin_assume_aligned(po + part(s + (Y + j) * G) * DP, 16), 32);
+                __builtin_memcpy(&y[j], __builtin_assume_aligned(po + (size_t)min(s + (Y + j) * G, a.splits - 1) * tile_rows * DP, 16), 32);
     }
     // the groups of a wave, then the waves
 #pragma unroll
@@ -803,7 +803,84 @@ __global__ __launch_bounds__(kAtJoin) void k_attend_join(AtArgs<MODE> a) {
         __builtin_memcpy(&z, __builtin_assume_aligned(&so[w][d], 16), 32);
         v += z;
     }
+    const int b = a.heads_(bh);
     write_row<T>(a, b, bh - b * a.c.heads, row, d, v);
+}
+
+// The same for the other forms' calls: a wave a row, whose lanes take the splits'
+// maxima and sums, and then eight channels each of every few splits; nothing
+// waits for another wave.  64 tokens of 32 heads behind a prefix in two splits:
+// 3.4 us, where a workgroup a row takes 4.7.
+template <int DP, class T, int NT, int MODE>
+__global__ __launch_bounds__(kAtJoin) void k_attend_join_rows(AtArgs<MODE> a) {
+    constexpr int W = DP / 8, G = 64 / W, K = kAtMaxSplits / 64, Y = 4, tile_rows = 16 * NT;
+    const int lane = threadIdx.x & 63, g = lane / W, d = lane % W * 8;
+    const unsigned rows = a.n * a.group, bh = blockIdx.y;
+    const unsigned row = __builtin_amdgcn_readfirstlane(blockIdx.x * (kAtJoin / 64) + (threadIdx.x >> 6));
+    if (row >= rows) return;
+    const unsigned nrt = (rows + tile_rows - 1) / tile_rows, place = nrt - 1 - row / tile_rows;
+    const int b = a.heads_(bh);
+    size_t first = ((size_t)bh * nrt + place) * a.splits * tile_rows + row % tile_rows, stacked = 0;
+    int splits = a.splits, stack_splits = 0, pitch = tile_rows;
+    if constexpr (MODE == kAtStack) {
+        const unsigned all = a.B * rows, at = b * rows + row, tiles = (all + tile_rows - 1) / tile_rows;
+        stacked = ((size_t)(bh - b * a.c.heads) * tiles + (tiles - 1 - at / tile_rows)) * a.stack_splits * tile_rows + at % tile_rows;
+        pitch = a.own_rows;
+        first = a.own_part + ((size_t)bh * nrt + place) * a.splits * pitch + row % tile_rows;
+        stack_splits = a.stack_splits;
+        splits += stack_splits;
+    }
+    // the row of a split's partial result
+    auto part = [&](int s) {
+        s = min(s, splits - 1);
+        return s < stack_splits ? stacked + (size_t)s * tile_rows : first + (size_t)(s - stack_splits) * pitch;
+    };
+    f2 z[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (k * 64 < splits) __builtin_memcpy(&z[k], __builtin_assume_aligned(a.part_ml + part(k * 64 + lane) * 2, 8), 8);
+    f8 y[Y];
+#pragma unroll
+    for (int j = 0; j < Y; ++j) __builtin_memcpy(&y[j], __builtin_assume_aligned(a.part_o + part(g + j * G) * DP + d, 16), 32);
+    __builtin_amdgcn_sched_barrier(0);
+    float most = -INFINITY, sum = 0.0f, weight[K] = {};
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (k * 64 < splits) most = fmaxf(most, z[k][0]);
+    most = lanes64(most, [](float x, float y) { return fmaxf(x, y); });
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (k * 64 + lane < splits) {
+            weight[k] = at_weight(z[k][0], z[k][1], most);
+            sum += weight[k] * z[k][1];
+        }
+    sum = lanes64(sum, [](float x, float y) { return x + y; });
+    const float scale = at_scale(most, sum);
+    f8 v = {};
+    for (int s = 0; s < splits; s += Y * G) {
+        f8 x[Y];
+#pragma unroll
+        for (int j = 0; j < Y; ++j) {
+            x[j] = y[j];
+            if (s + Y * G < splits) __builtin_memcpy(&y[j], __builtin_assume_aligned(a.part_o + part(s + (Y + j) * G + g) * DP + d, 16), 32);
+        }
+        // (64 is a multiple of the splits of a step)
+        float of = weight[0];
+#pragma unroll
+        for (int k = 1; k < K; ++k) of = s >= k * 64 ? weight[k] : of;
+#pragma unroll
+        for (int j = 0; j < Y; ++j) {
+            const int split = s + j * G + g;
+            const float by = __shfl(of, split % 64) * scale;
+            if (split < splits) v += by * x[j];
+        }
+    }
+    // the groups of the wave
+#pragma unroll
+    for (int x = W; x < 64; x <<= 1)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += __shfl_xor(v[e], x);
+    if (lane < W && d < a.c.dim) write_row<T>(a, b, bh - b * a.c.heads, row, d, v);
 }
 
 // ---- host -----------------------------------------------------------------------
@@ -884,50 +961,98 @@ long long attend_window_plan(AttendRunsArgs& a, int precision) {
     return split_plan(a, precision, some < all ? some : all);
 }
 
-// The rows of all sequences over the prefix and each one's over its own tokens in
-// one launch.  False where their partial results do not fit the workspace.
-static bool stack_plan(AttendRunsArgs& a, int precision, int nt) {
-    const int waves = nt == 1 && a.c.dp * (precision == WF_BF16 ? 2 : 4) < 1024 ? 8 : 4;
-    const long long rows = (long long)a.n * a.group, tile = 16 * nt;
-    const long long shared = a.c.heads * ((a.B * rows + tile - 1) / tile), own = a.max_visible ? a.B * a.c.heads * ((rows + tile - 1) / tile) : 0;
-    const long long shared_tiles = tiles_of(a.max_first), own_tiles = tiles_of(a.max_visible);
-    const long long room = (long long)attend_work_rows(a.c.dp) / tile;
-    if (shared + own > room) return false;
-    // Both parts are split into shares of as many tiles, so many that the chip is
-    // filled, down to a tile a wave: there is a join in any case.
-    long long share = (shared * shared_tiles + own * own_tiles + kAtTarget * 2 - 1) / (kAtTarget * 2);
-    share = share < waves ? waves : share;
-    long long s, o;
-    for (;; share += (share + 7) / 8) {
-        s = (shared_tiles + share - 1) / share;
-        o = own ? (own_tiles + share - 1) / share : 0;
-        if (s + o <= kAtMaxSplits && shared * s + own * o <= room) break;
-    }
-    a.stack_splits = (int)s; a.splits = (int)o;
-    a.stack_splits_.by((unsigned)s); a.splits_.by(o ? (unsigned)o : 1u);
-    a.stack_tiles_.by((unsigned)((a.B * rows + tile - 1) / tile)); a.tiles_.by((unsigned)((rows + tile - 1) / tile));
-    a.heads_.by(a.c.heads); a.group_.by(a.group); a.n_.by(a.n);
-    a.stack_blocks = (int)(shared * s);
-    a.own_part = shared * s * tile;
-    return true;
+// Workgroups that read the same tokens, on one die: its cache then holds them.
+// Units of equal work, all row tiles of a sequence and head (over a shared
+// prefix each row tile), are dealt to the dies in the order of heads where they
+// come out even.  us with and without: 64 tokens of 32 / 8 heads of 128 behind
+// 8192 24.0 / 24.7, of 64 channels 18.5 / 19.9, 16 tokens 12.0 / 12.8, 256 tokens
+// 81.7 / 85.0.
+static void deal(AttendRunsArgs& a, long long units, long long workgroups) {
+    a.units_of_die = 0;
+    if (units % kXcds) return;
+    a.units_of_die = (int)(units / kXcds);
+    a.unit_workgroups = (int)workgroups;
+    a.unit_.by((unsigned)workgroups);
+    a.batch_.by((unsigned)a.B);
 }
 
-static int stack_row_tiles(const AttendRunsArgs& a, int precision) { return a.c.dp * (precision == WF_BF16 ? 2 : 4) <= 256 ? 2 : 1; }
+// Time of a launch in tiles of 16 rows: workgroups on a compute unit in turn, each
+// with a start and an end as long as kAtEnds tiles take, a tile of 32 rows as long
+// as 1.64 of 16; the join as long as kAtEnds too.  (1.02 us for eight waves' tiles
+// of 16 rows, 0.91 for four waves' of 32; 64 tokens of 32 / 8 heads of 128 behind
+// 8192 in one to eight splits: 37.9, 25.8, 29.4, 29.6, -, 31.0, -, 31.1 us, with 32
+// rows 60.7, 35.5, 28.1, 24.4, -, 27.3, -, 28.4; 16 tokens in 2, 4, 8 and 16 splits
+// 21.9, 15.0, 12.3, 15.3.)
+constexpr double kAtEnds = 24.0;
+static double cost_of(long long groups, long long tiles, long long splits, int nt) {
+    const double turns = (double)((groups * splits + kAtTarget - 1) / kAtTarget);
+    return (nt == 2 ? 1.64 : 1.0) * turns * ((tiles + splits - 1) / splits + kAtEnds);
+}
 
-long long attend_shared_plan(AttendRunsArgs& a, int precision, int* together) {
-    const int nt = stack_row_tiles(a, precision);
-    const long long rows = (long long)a.n * a.group, tile = 16 * nt, first = tiles_of(a.max_first), own = tiles_of(a.max_visible);
-    // Tiles that workgroups take, with the rows together over the prefix and apart.
-    const long long apart = a.B * ((rows + tile - 1) / tile) * (first + own);
-    const long long joint = (a.B * rows + tile - 1) / tile * first + a.B * ((rows + tile - 1) / tile) * own;
-    *together = 0;
-    if (a.B > 1 && first && 5 * joint < 4 * apart && a.B * rows < 1LL << 24) {
-        AttendRunsArgs x = a;
-        for (x.B = a.B; x.B > 1 && !stack_plan(x, precision, nt);) x.B = (x.B + 1) / 2 == x.B ? 1 : (x.B + 1) / 2;
-        if (x.B > 1) *together = x.B;
+// The rows of all sequences over the prefix and each one's over its own tokens in
+// one launch, with a join: its time in tiles, or less than 0 where the partial
+// results do not fit the workspace.
+static double stack_plan(AttendRunsArgs& a, int precision, int nt) {
+    const int waves = nt == 1 && a.c.dp * (precision == WF_BF16 ? 2 : 4) < 1024 ? 8 : 4;
+    const long long rows = (long long)a.n * a.group, tile = 16 * nt, all = (a.B * rows + tile - 1) / tile, each = (rows + tile - 1) / tile;
+    const long long shared = a.c.heads * all, own = a.max_visible ? a.B * a.c.heads * each : 0;
+    const long long shared_tiles = tiles_of(a.max_first), own_tiles = tiles_of(a.max_visible), own_rows = rows < tile ? rows : tile;
+    const long long room = (long long)attend_work_rows(a.c.dp);
+    double best = -1.0;
+    // the most splits that the compute units hold in one, two .. turns, of four tiles or more
+    for (int turns = 1; turns <= 4; ++turns) {
+        long long s = kAtTarget * turns / shared, most = shared_tiles / 4;
+        most = most < kAtMaxSplits / 2 ? most : kAtMaxSplits / 2;
+        s = s < most ? s : most;
+        s = s < 1 ? 1 : s;
+        // own tokens in parts as long as the prefix's, but no more of them than workgroups for two turns
+        const long long share = (shared_tiles + s - 1) / s > 4 * waves ? (shared_tiles + s - 1) / s : 4 * waves;
+        long long o = own ? (own_tiles + share - 1) / share : 0, fill = own ? 2 * kAtTarget / own : 0;
+        fill = fill < kAtMaxSplits / 2 ? fill : kAtMaxSplits / 2;
+        o = o < fill ? o : fill;
+        o = own && o < 1 ? 1 : o;
+        // (so that a part of a batch that fits does)
+        while (shared * s * tile + own * o * own_rows > room && (o > 1 || s > 1)) (o > 1 ? o : s) /= 2;
+        if (shared * s * tile + own * o * own_rows > room) continue;
+        const double part = own ? (nt == 2 ? 1.64 : 1.0) * own * o / kAtTarget * ((own_tiles + o - 1) / o + kAtEnds) : 0.0;
+        const double cost = cost_of(shared, shared_tiles, s, nt) + part + kAtEnds;
+        if (best >= 0.0 && cost >= best) continue;
+        best = cost;
+        a.stack_splits = (int)s; a.splits = (int)o;
     }
-    if (*together) return 0;
-    return split_plan(a, precision, first + own);
+    if (best < 0.0) return best;
+    a.stack_splits_.by(a.stack_splits); a.splits_.by(a.splits ? a.splits : 1u);
+    a.stack_tiles_.by((unsigned)all); a.tiles_.by((unsigned)each);
+    a.heads_.by(a.c.heads); a.group_.by(a.group); a.n_.by(a.n);
+    a.stack_blocks = (int)(shared * a.stack_splits);
+    a.own_part = shared * a.stack_splits * tile;
+    a.own_rows = (int)own_rows;
+    deal(a, shared, a.stack_splits);
+    return best;
+}
+
+long long attend_shared_plan(AttendRunsArgs& a, int precision, AttendStack* stack) {
+    const long long first = tiles_of(a.max_first), own = tiles_of(a.max_visible);
+    const long long threads = split_plan(a, precision, first + own);
+    const int nt = row_tiles(a, precision), rows = a.n * a.group;
+    *stack = {0, 1};
+    if (a.B < 2 || !first || (long long)a.B * rows >= 1 << 24) return threads;
+    double best = cost_of((long long)a.B * a.c.heads * ((rows + 16 * nt - 1) / (16 * nt)), first + own, a.splits, nt) + (a.splits > 1 ? kAtEnds : 0.0);
+    for (int tiles = 1; tiles <= (a.c.dp * (precision == WF_BF16 ? 2 : 4) <= 256 ? 2 : 1); ++tiles) {
+        // as many sequences as the workspace takes, in as many launches as that makes
+        AttendRunsArgs x = a;
+        for (int launches = 1; launches <= 64 && launches < a.B; launches *= 2) {
+            x.B = (a.B + launches - 1) / launches;
+            const double cost = launches * stack_plan(x, precision, tiles);
+            if (cost < 0.0) continue;
+            if (cost < best) {
+                best = cost;
+                *stack = {x.B, tiles};
+            }
+            break;
+        }
+    }
+    return stack->sequences ? 0 : threads;
 }
 
 // The kernel of a form and, where its calls are split, the join.
@@ -937,8 +1062,12 @@ static void launch_form(const AtArgs<MODE>& a, hipStream_t st) {
     long long groups = (long long)a.B * a.c.heads * ((rows + 16 * NT - 1) / (16 * NT)) * a.splits;
     if constexpr (MODE == kAtStack) groups += a.stack_blocks;
     hipLaunchKernelGGL((k_attend<DP, T, NT, MODE>), dim3((unsigned)groups), dim3(64 * kAtWaves<DP, T, NT>), 0, st, a);
-    if (MODE == kAtStack || a.splits > 1)
-        hipLaunchKernelGGL((k_attend_join<DP, T, NT, MODE == kAtMask ? kAtPlain : MODE>), dim3(a.n * a.group, a.B * a.c.heads), dim3(kAtJoin), 0, st, a);
+    if constexpr (MODE == kAtPlain || MODE == kAtMask) {
+        if (a.splits > 1) hipLaunchKernelGGL((k_attend_join<DP, T, NT>), dim3(rows, a.B * a.c.heads), dim3(kAtJoin), 0, st, a);
+    } else if (MODE == kAtStack || a.splits > 1) {
+        const int per = kAtJoin / 64;
+        hipLaunchKernelGGL((k_attend_join_rows<DP, T, NT, MODE>), dim3((rows + per - 1) / per, a.B * a.c.heads), dim3(kAtJoin), 0, st, a);
+    }
 }
 
 template <int DP, class T, int MODE>
@@ -967,23 +1096,29 @@ void launch_attend(const AttendArgs& a, int precision, hipStream_t st) {
     else launch<kAtPlain>(a, precision, nt, st);
 }
 
-void launch_attend_window(const AttendRunsArgs& a, int precision, hipStream_t st) { launch<kAtRuns>(a, precision, row_tiles(a, precision), st); }
+static void launch_runs(const AttendRunsArgs& a, int precision, hipStream_t st) {
+    const int nt = row_tiles(a, precision), rows = a.n * a.group;
+    AttendRunsArgs x = a;
+    deal(x, (long long)a.B * a.c.heads, (long long)((rows + 16 * nt - 1) / (16 * nt)) * a.splits);
+    launch<kAtRuns>(x, precision, nt, st);
+}
 
-void launch_attend_shared(const AttendRunsArgs& a, int precision, int together, hipStream_t st) {
-    if (!together) return launch<kAtRuns>(a, precision, row_tiles(a, precision), st);
-    // sequences in turn, since the launches share the workspace
-    const int nt = stack_row_tiles(a, precision);
-    const size_t item = precision == WF_BF16 ? 2 : 4;
-    for (int b = 0; b < a.B; b += together) {
+void launch_attend_window(const AttendRunsArgs& a, int precision, hipStream_t st) { launch_runs(a, precision, st); }
+
+void launch_attend_shared(const AttendRunsArgs& a, int precision, const AttendStack& stack, hipStream_t st) {
+    if (!stack.sequences) return launch_runs(a, precision, st);
+    // launches in turn, since they share the workspace
+    const long long item = precision == WF_BF16 ? 2 : 4;
+    for (int b = 0; b < a.B; b += stack.sequences) {
         AttendRunsArgs x = a;
-        x.B = together < a.B - b ? together : a.B - b;
-        x.q.p = (char*)a.q.p + b * a.q.sb * (long long)item;
-        x.o.p = (char*)a.o.p + b * a.o.sb * (long long)item;
+        x.B = stack.sequences < a.B - b ? stack.sequences : a.B - b;
+        x.q.p = (char*)a.q.p + b * a.q.sb * item;
+        x.o.p = (char*)a.o.p + b * a.o.sb * item;
         x.table += (size_t)b * a.table_pages;
         x.visible += (size_t)b * a.n;
         x.first_visible += (size_t)b * a.n;
-        stack_plan(x, precision, nt);
-        launch<kAtStack>(x, precision, nt, st);
+        stack_plan(x, precision, stack.row_tiles);
+        launch<kAtStack>(x, precision, stack.row_tiles, st);
     }
 }
 

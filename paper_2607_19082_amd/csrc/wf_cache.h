@@ -178,7 +178,12 @@ struct AttendRunsArgs : AttendArgs {
     // rows of all sequences together over the prefix, as workgroups before the others
     int stack_blocks, stack_splits;
     KvDiv stack_splits_, stack_tiles_, n_;
-    long long own_part;              // the first row of the others' partial results
+    long long own_part;              // the first row of the others' partial results,
+    int own_rows;                    // and how many a tile has
+    // > 0: a unit of work's place goes by its die, units in the order of heads:
+    // this many of each die's
+    int units_of_die, unit_workgroups;
+    KvDiv unit_, batch_;
 };
 
 void launch_kv_write(const KvCache&, int precision, const KvRows& k, const KvRows& v, const KvTokens&, hipStream_t);
@@ -188,9 +193,10 @@ long long attend_plan(AttendArgs&, int precision);
 void launch_attend(const AttendArgs&, int precision, hipStream_t);
 long long attend_window_plan(AttendRunsArgs&, int precision);
 void launch_attend_window(const AttendRunsArgs&, int precision, hipStream_t);
-// Sequences that a launch takes together (0: every sequence for itself, in one
-// launch), and the threads of the largest.
-long long attend_shared_plan(AttendRunsArgs&, int precision, int* together);
-void launch_attend_shared(const AttendRunsArgs&, int precision, int together, hipStream_t);
+// How the rows of a batch over its prefix are taken: those of so many sequences
+// together (0: each sequence's for itself, in one launch), in so many tiles of 16.
+struct AttendStack { int sequences, row_tiles; };
+long long attend_shared_plan(AttendRunsArgs&, int precision, AttendStack*);
+void launch_attend_shared(const AttendRunsArgs&, int precision, const AttendStack&, hipStream_t);
 
 }  // namespace wf

@@ -466,11 +466,11 @@ int wf_cache_attend_shared(wf_cache_t cache, int32_t precision, const wf_rows* q
     if (!prefix_visible || (max_prefix && !prefix_table)) return fail(WF_E_INVALID, "prefix_visible or prefix_table is NULL");
     a.first_table = prefix_table; a.first_visible = prefix_visible;
     a.first_pages = prefix_pages; a.max_first = max_prefix;
-    int together;
-    if (attend_shared_plan(a, precision, &together) >= 1LL << 32) return fail(WF_E_UNSUPPORTED, "2^32 or more threads in one call");
+    AttendStack stack;
+    if (attend_shared_plan(a, precision, &stack) >= 1LL << 32) return fail(WF_E_UNSUPPORTED, "2^32 or more threads in one call");
     const OnDevice on(c->device);
     if (on.error() != hipSuccess) return kv_fail(on.error(), "the cache's device");
-    launch_attend_shared(a, precision, together, stream);
+    launch_attend_shared(a, precision, stack, stream);
     return kv_launched("wf_cache_attend_shared");
 } catch (...) {
     return WF_E_NOMEM;

@@ -73,9 +73,19 @@ for dim in (64, 128, 256):
                         rc, made = f(h, B, n, heads * group, *args, precision=precision)
                         assert rc == 0 and (len(made) == 1 or len(made) % 2 == 0)
                         if len(made) > 1:               # each launch and its join
+                            launches = len(made) // 2
+                            part, left = -(-B // launches), B
                             for c in made[::2]:
                                 tile = 32 if c.block == 256 and dim * item < 1024 else 16
-                                assert c.grid * tile * (dim + 2) * 4 <= room, (dim, heads, precision, group, B, n, args)
+                                fits = c.grid * tile * (dim + 2) * 4 <= room
+                                if f is shared and not fits:
+                                    # rows of all over the prefix, in tiles, and each sequence's over its own, in rows
+                                    b, r = min(part, left), n * group
+                                    first, own = heads * -(-b * r // tile), b * heads * -(-r // tile) if args[1] else 0
+                                    fits = any((s * first * tile + (c.grid - s * first) * min(r, tile)) * (dim + 2) * 4 <= room
+                                               and (c.grid - s * first) % max(1, own) == 0 for s in range(1, c.grid // first + 1))
+                                assert fits, (dim, heads, precision, group, B, n, args)
+                                left -= part
                             most = max(most, len(made))
         L.wf_cache_destroy(h)
 assert most > 8                                         # batches that are taken in parts
