@@ -23,6 +23,10 @@ namespace wf {
 
 constexpr int kNormThreads = 256;
 constexpr int kNormPairs = 128;      // of a head, at most
+// Outputs of more bytes than the second-level caches hold are stored past them:
+// 2 x 8191 tokens of 40 heads of 128 in bf16 (321 MB both ways) 76 us, through
+// them 81; shorter ones stay where the next kernel finds them.
+constexpr long long kNormStream = 32 << 20;
 
 struct NormArgs {
     KvRows x[2], y[2];               // queries, keys: in, out
@@ -78,10 +82,19 @@ __device__ __forceinline__ double head_sum(double x) {
     return x;
 }
 
+template <int N, bool STREAM, class T>
+__device__ __forceinline__ void store(T* p, const T* x) {
+    typedef unsigned Words __attribute__((ext_vector_type(N * sizeof(T) / 4), aligned(sizeof(T))));
+    Words w;
+    __builtin_memcpy(&w, x, sizeof w);
+    if constexpr (STREAM) __builtin_nontemporal_store(w, (Words*)p);
+    else *(Words*)p = w;
+}
+
 // The four pairs of a unit: NEIGHBOURS pairs channels 2 j and 2 j + 1, and the
 // unit's eight lie together; else the pair's second channel is half of the
-// axis's channels on.
-template <class T, int LPH, bool NEIGHBOURS>
+// axis's channels on.  STREAM: stores past the caches.
+template <class T, int LPH, bool NEIGHBOURS, bool STREAM>
 __global__ __launch_bounds__(kNormThreads) void k_head_norm(NormArgs a) {
     constexpr int kHeads = 64 / LPH;     // of a wave at once, of one token or several
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -164,10 +177,10 @@ __global__ __launch_bounds__(kNormThreads) void k_head_norm(NormArgs a) {
             T* p = key ? (T*)a.y[1].p + b * a.y[1].sb + i * a.y[1].sr + (h - a.q_heads) * a.y[1].sh
                        : (T*)a.y[0].p + b * a.y[0].sb + i * a.y[0].sr + h * a.y[0].sh;
             if constexpr (NEIGHBOURS) {
-                __builtin_memcpy(p + at[0], out, sizeof out);
+                store<8, STREAM>(p + at[0], out);
             } else {
-                __builtin_memcpy(p + at[0], out, sizeof out / 2);
-                __builtin_memcpy(p + at[1], out + 4, sizeof out / 2);
+                store<4, STREAM>(p + at[0], out);
+                store<4, STREAM>(p + at[1], out + 4);
             }
         }
 #pragma unroll
@@ -209,18 +222,25 @@ static long long norm_plan(NormArgs& a, int lph) {
     return g * a.chunks;
 }
 
-template <class T, int LPH>
-static void launch_norm(const NormArgs& a, bool neighbours, long long waves, hipStream_t st) {
+template <class T, int LPH, bool NEIGHBOURS>
+static void launch_norm(const NormArgs& a, long long waves, hipStream_t st) {
     const dim3 grid((unsigned)((waves + kNormThreads / 64 - 1) / (kNormThreads / 64)));
-    if (neighbours) hipLaunchKernelGGL((k_head_norm<T, LPH, true>), grid, dim3(kNormThreads), 0, st, a);
-    else hipLaunchKernelGGL((k_head_norm<T, LPH, false>), grid, dim3(kNormThreads), 0, st, a);
+    const bool stream = (long long)a.tokens * a.heads * a.dim * (long long)sizeof(T) > kNormStream;
+    if (stream) hipLaunchKernelGGL((k_head_norm<T, LPH, NEIGHBOURS, true>), grid, dim3(kNormThreads), 0, st, a);
+    else hipLaunchKernelGGL((k_head_norm<T, LPH, NEIGHBOURS, false>), grid, dim3(kNormThreads), 0, st, a);
+}
+
+template <class T, int LPH>
+static void launch_norm_pairs(const NormArgs& a, bool neighbours, long long waves, hipStream_t st) {
+    if (neighbours) launch_norm<T, LPH, true>(a, waves, st);
+    else launch_norm<T, LPH, false>(a, waves, st);
 }
 
 template <class T>
 static void launch_norm_dim(const NormArgs& a, bool neighbours, int lph, long long waves, hipStream_t st) {
-    if (lph == 8) launch_norm<T, 8>(a, neighbours, waves, st);
-    else if (lph == 16) launch_norm<T, 16>(a, neighbours, waves, st);
-    else launch_norm<T, 32>(a, neighbours, waves, st);
+    if (lph == 8) launch_norm_pairs<T, 8>(a, neighbours, waves, st);
+    else if (lph == 16) launch_norm_pairs<T, 16>(a, neighbours, waves, st);
+    else launch_norm_pairs<T, 32>(a, neighbours, waves, st);
 }
 
 }  // namespace wf
