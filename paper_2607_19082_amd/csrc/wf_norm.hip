@@ -14,6 +14,13 @@
 // Angles are fixed-point turns: position times frequency, modulo one turn, is
 // the low 64 bits of a product of integers, exact but for the frequency's own
 // rounding to 2^-64 of a turn.  A position of 2^31 is as exact as one of 1.
+//
+// Bound by memory where there are many tokens (MI355X): 2 x 8191 tokens of 32
+// query and 8 key heads of 128 in bf16, 321 MB both ways with the second
+// sequence shorter, 75 us, 4.3 TB/s where a large copy reaches 4.6; vector
+// instructions take 53% of the time beside it.  Heads in turn share a lane's
+// sines, which would otherwise cost more than the rest.  A token 3.9 us, a
+// launch and its chain of loads.
 #include <cmath>
 #include <new>
 
@@ -190,7 +197,10 @@ __global__ __launch_bounds__(kNormThreads) void k_head_norm(NormArgs a) {
 
 // ---- host -----------------------------------------------------------------------
 
-constexpr int kNormFill = 4096;      // waves that fill the chip
+// Waves that fill the chip: fewer heads each make more sines and shorter runs.  us
+// at 2048 / 4096 / 8192 / 16384: a 4K grid's 10 fp32 heads of 64 39.7 / 40.0 /
+// 45.8 / 49.6, the prompts above 80.9 / 81.3 / 81.0 / 86.3 (through the caches).
+constexpr int kNormFill = 4096;
 
 struct HeadNorm {
     int device = 0;
