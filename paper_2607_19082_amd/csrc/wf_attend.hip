@@ -413,7 +413,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     // most of the second's first tokens, that a row sees
     int least_first = 0, most_first = 0, low = 0, high = 0;
     if constexpr (RUNS) {
-        least_first = a.max_first;
+        least_first = a.window ? a.sinks : a.max_first;
         low = max_visible;
     }
 #pragma unroll

@@ -182,7 +182,7 @@ def test_shared(B, n, heads, group, P, L, causal, dim, dtype):
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("dim,B,n,heads,group,P,L,page", [
     (128, 64, 1, 8, 4, 4097, 70, 64), (64, 16, 45, 5, 1, 3001, 90, 64), (128, 8, 64, 2, 4, 2050, 64, 32), (256, 30, 1, 1, 8, 9001, 5, 1024),
-    (64, 100, 3, 2, 1, 700, 1500, 128), (96, 2, 300, 8, 2, 500, 300, 64), (8, 700, 1, 4, 2, 333, 40, 32), (128, 3, 1, 2, 1, 20011, 9000, 64)])
+    (64, 100, 3, 2, 1, 700, 1500, 128), (96, 2, 300, 8, 2, 500, 300, 64), (8, 700, 1, 4, 2, 333, 40, 32), (8, 3000, 1, 4, 2, 200, 5, 32), (128, 3, 1, 2, 1, 20011, 9000, 64)])
 def test_shared_long(dim, B, n, heads, group, P, L, page, dtype):
     """Prefixes split over workgroups, more rows than one launch's workspace
     holds, own tokens that are longer than the prefix; unequal rows."""
