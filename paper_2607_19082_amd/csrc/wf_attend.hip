@@ -41,8 +41,8 @@
 // The other forms take the same tiles from other lists.  With a window a tile of
 // rows goes over its rows' first tokens and from the first token that one of them
 // sees: 64 tokens with windows of 1024 in 0 to 8192 15 us (4.1 TB/s), 1024 rows
-// with windows of 4096 102 (0.68 PFLOP/s).  Behind a shared prefix each row goes
-// over that and its own tokens (8 x 128 rows behind 16384 362 us, 0.76 PFLOP/s),
+// with windows of 4096 100 (0.69 PFLOP/s).  Behind a shared prefix each row goes
+// over that and its own tokens (8 x 128 rows behind 16384 352 us, 0.78 PFLOP/s),
 // or, where sequences have few rows, those of all sequences fill the tiles over
 // the prefix together: 64 tokens behind 8192, 32 / 8 heads, 24 us, where 64 times
 // the prefix takes 68.
@@ -917,8 +917,9 @@ static int row_tiles(const AttendArgs& a, int precision) {
     return rows > 16 && tiles * a.c.dp >= kAtManyRows && a.c.dp * (precision == WF_BF16 ? 2 : 4) <= 256 ? 2 : 1;
 }
 
-// How the tiles of a workgroup's rows are split.  Returns the threads of the launch.
-static long long split_plan(AttendArgs& a, int precision, long long tiles) {
+// How the tiles of a workgroup's rows are split: not where they are so few a
+// wave.  Returns the threads of the launch.
+static long long split_plan(AttendArgs& a, int precision, long long tiles, int few) {
     const int bytes = a.c.dp * (precision == WF_BF16 ? 2 : 4), nt = row_tiles(a, precision), rows = a.n * a.group;
     const int waves = nt == 1 && bytes < 1024 ? 8 : 4;
     const long long groups = (long long)a.B * a.c.heads * ((rows + 16 * nt - 1) / (16 * nt));
@@ -927,7 +928,7 @@ static long long split_plan(AttendArgs& a, int precision, long long tiles) {
     // tiles each, two and one: a token over 1001 (8 heads of 128, bf16) 7.3, 7.4,
     // 8.3, 7.4, over 2047 11.0, 10.2, 8.5, 7.8, over 8192 33, 10.6, 9.1, 8.7; 45
     // fp32 rows over 1024 7.2, 7.2, 8.5, 7.8, over 4096 16.9, 10.7, 9.0, 8.5.
-    const long long by_len = tiles <= 4 * waves ? 1 : (tiles + waves - 1) / waves;
+    const long long by_len = tiles <= few * waves ? 1 : (tiles + waves - 1) / waves;
     long long s = kAtTarget / groups;
     // Long calls (8192 tokens) that would leave many compute units idle take two
     // workgroups each where that fills a fifth more: us without and with, 8 key
@@ -958,7 +959,7 @@ static long long tiles_of(long long tokens) { return (tokens + kKvTile - 1) / kK
 long long attend_plan(AttendArgs& a, int precision) {
     const int bytes = a.c.dp * (precision == WF_BF16 ? 2 : 4), nt = row_tiles(a, precision), rows = a.n * a.group;
     const long long groups = (long long)a.B * a.c.heads * ((rows + 16 * nt - 1) / (16 * nt));
-    const long long threads = split_plan(a, precision, tiles_of(a.max_visible));
+    const long long threads = split_plan(a, precision, tiles_of(a.max_visible), 4);
     // A token each of sequences that may be of unequal lengths, and two
     // workgroups on most compute units.  With more of them the units take the
     // next as they finish: in the order given and longest first, 128 sequences
@@ -969,12 +970,19 @@ long long attend_plan(AttendArgs& a, int precision) {
     return threads;
 }
 
+// The other forms' calls are split from a tile a wave later: a second launch is 3
+// us of the host, which a call waits for that no graph holds.  us with and
+// without a split, a call after another and (from a graph): a token, 38 tiles,
+// 10.6 / 9.6 (8.0 / 9.4), 45 fp32 rows, 33 tiles 10.8 / 8.1 (8.3 / 8.1), 38 tiles
+// 10.5 / 8.9 (8.3 / 9.0); 46 tiles 10.5 / 10.4 (8.0 / 10.3).
+constexpr int kAtFew = 5;
+
 // A window's rows read its tokens, those that the other rows of their tile are
 // ahead by under a causal order, and the first tokens.
 long long attend_window_plan(AttendRunsArgs& a, int precision) {
     const int rows = 16 * row_tiles(a, precision), apart = (rows + a.group - 1) / a.group, ahead = (apart < a.n ? apart : a.n) - 1;
     const long long all = tiles_of(a.max_visible), some = tiles_of(a.sinks) + tiles_of((long long)a.window + ahead) + 1;
-    return split_plan(a, precision, some < all ? some : all);
+    return split_plan(a, precision, some < all ? some : all, kAtFew);
 }
 
 // Workgroups that read the same tokens, on one die: its cache then holds them.
@@ -994,12 +1002,13 @@ static void deal(AttendRunsArgs& a, long long units, long long workgroups) {
 
 // Time of a launch in tiles of 16 rows: workgroups on a compute unit in turn, each
 // with a start and an end as long as kAtEnds tiles take, a tile of 32 rows as long
-// as 1.64 of 16; the join as long as kAtEnds too.  (1.02 us for eight waves' tiles
+// as 1.64 of 16; the join as long as kAtEnds too, and its launch kAtLaunch where
+// the host is what a call waits for.  (1.02 us for eight waves' tiles
 // of 16 rows, 0.91 for four waves' of 32; 64 tokens of 32 / 8 heads of 128 behind
 // 8192 in one to eight splits: 37.9, 25.8, 29.4, 29.6, -, 31.0, -, 31.1 us, with 32
 // rows 60.7, 35.5, 28.1, 24.4, -, 27.3, -, 28.4; 16 tokens in 2, 4, 8 and 16 splits
 // 21.9, 15.0, 12.3, 15.3.)
-constexpr double kAtEnds = 24.0;
+constexpr double kAtEnds = 24.0, kAtLaunch = 12.0;
 static double cost_of(long long groups, long long tiles, long long splits, int nt) {
     const double turns = (double)((groups * splits + kAtTarget - 1) / kAtTarget);
     return (nt == 2 ? 1.64 : 1.0) * turns * ((tiles + splits - 1) / splits + kAtEnds);
@@ -1031,7 +1040,7 @@ static double stack_plan(AttendRunsArgs& a, int precision, int nt) {
         while (shared * s * tile + own * o * own_rows > room && (o > 1 || s > 1)) (o > 1 ? o : s) /= 2;
         if (shared * s * tile + own * o * own_rows > room) continue;
         const double part = own ? (nt == 2 ? 1.64 : 1.0) * own * o / kAtTarget * ((own_tiles + o - 1) / o + kAtEnds) : 0.0;
-        const double cost = cost_of(shared, shared_tiles, s, nt) + part + kAtEnds;
+        const double cost = cost_of(shared, shared_tiles, s, nt) + part + kAtEnds + kAtLaunch;
         if (best >= 0.0 && cost >= best) continue;
         best = cost;
         a.stack_splits = (int)s; a.splits = (int)o;
@@ -1049,11 +1058,11 @@ static double stack_plan(AttendRunsArgs& a, int precision, int nt) {
 
 long long attend_shared_plan(AttendRunsArgs& a, int precision, AttendStack* stack) {
     const long long first = tiles_of(a.max_first), own = tiles_of(a.max_visible);
-    const long long threads = split_plan(a, precision, first + own);
+    const long long threads = split_plan(a, precision, first + own, kAtFew);
     const int nt = row_tiles(a, precision), rows = a.n * a.group;
     *stack = {0, 1};
     if (a.B < 2 || !first || (long long)a.B * rows >= 1 << 24) return threads;
-    double best = cost_of((long long)a.B * a.c.heads * ((rows + 16 * nt - 1) / (16 * nt)), first + own, a.splits, nt) + (a.splits > 1 ? kAtEnds : 0.0);
+    double best = cost_of((long long)a.B * a.c.heads * ((rows + 16 * nt - 1) / (16 * nt)), first + own, a.splits, nt) + (a.splits > 1 ? kAtEnds + kAtLaunch : 0.0);
     for (int tiles = 1; tiles <= (a.c.dp * (precision == WF_BF16 ? 2 : 4) <= 256 ? 2 : 1); ++tiles) {
         // as many sequences as the workspace takes, in as many launches as that makes
         AttendRunsArgs x = a;
