@@ -326,9 +326,9 @@ __device__ __forceinline__ int by_length(const AttendArgs& a, int place, int ahe
     return __builtin_amdgcn_readfirstlane(found);
 }
 
-// One workgroup: 16 NT rows of a sequence's key head, and a share of its
-// tokens.
-template <int DP, class T, int NT, int MODE>
+// A team of TEAM waves (a workgroup's, as a rule): 16 NT rows of a sequence's key
+// head, and a share of its tokens.
+template <int DP, class T, int NT, int MODE, int TEAM = kAtWaves<DP, T, NT>>
 __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, NT>)) void k_attend(AtArgs<MODE> a) {
     constexpr bool MASK = MODE == kAtMask, RUNS = MODE == kAtRuns, STACK = MODE == kAtStack;
     // A wave at its values' products goes ahead of the SIMD's others.  us without
@@ -337,8 +337,11 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     // fp32 36.8 / 35.7; of 64 channels in fp32, two tiles of rows, 58.2 / 60.6.
     constexpr bool kAhead = (RUNS || STACK) && !(NT == 2 && sizeof(T) == 4);
     constexpr int NW = kAtWaves<DP, T, NT>, NQ = AtParts<T>::kQ, NP = AtParts<T>::kP, NK = DP / 32, ND = DP / 16;
+    constexpr int TEAMS = NW / TEAM;
+    static_assert(TEAMS == 1 || RUNS, "teams are of calls by runs");
     using L = KvLayout<DP>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
+    const int team = TEAMS == 1 ? 0 : wave / TEAM, member = TEAMS == 1 ? wave : wave % TEAM;
     // what the workgroup takes: a sequence's own tokens, or all sequences' rows
     // over the prefix as if they were one's
     int block = blockIdx.x, n = a.n, splits = a.splits, max_visible = a.max_visible, table_pages = a.table_pages;
@@ -357,6 +360,13 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
         }
     }
     const int rows = n * a.group, nrt = (rows + 16 * NT - 1) / (16 * NT);
+    bool idle = false;                                 // a team past the last
+    if constexpr (TEAMS > 1) {
+        block = a.units_of_die ? block / kXcds * TEAMS + team : block * TEAMS + team;      // of the die, or of all
+        idle = block >= (a.units_of_die ? a.units_of_die * a.unit_workgroups : a.B * a.c.heads * nrt);
+        block = idle ? 0 : block;
+        if (a.units_of_die) block = block * kXcds + blockIdx.x % kXcds;
+    }
     int group = splits_(block), split = block - group * splits;
     const int bh = tiles_(group);
     int place = group - bh * nrt, b = a.heads_(bh), head = bh - b * a.c.heads;
@@ -387,7 +397,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     // What the rows see, their queries, and the page that the wave begins with
     // if a row sees all it may: in flight together, since each waits as long as
     // a short call's whole arithmetic takes.
-    const int expect = RUNS ? -1 : (int)(splits_((max_visible + kKvTile - 1) / kKvTile + splits - 1) * split + wave) >> in_page;
+    const int expect = RUNS ? -1 : (int)(splits_((max_visible + kKvTile - 1) / kKvTile + splits - 1) * split + member) >> in_page;
     const int expected = !RUNS && max_visible ? table[min(expect, table_pages - 1)] : 0;
     int see[NT], most = 0, least = max_visible;
     int see_first[NT];                                 // kAtRuns: tokens of the first run,
@@ -397,7 +407,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const int row = rt * 16 * NT + t * 16 + col;
-        const bool on = row < rows;                    // a column past the last row repeats the first
+        const bool on = row < rows && !idle;           // a column past the last row repeats the first
         const int i = on ? a.group_(row) : 0, h = (head - i) * a.group + (on ? row : 0);
         see[t] = visible[(size_t)b * n + i];
         if constexpr (RUNS) see_first[t] = a.window ? 0 : a.first_visible[(size_t)b * n + i];
@@ -423,7 +433,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const bool on = rt * 16 * NT + t * 16 + col < rows;
+        const bool on = rt * 16 * NT + t * 16 + col < rows && !idle;
         if (on && see[t] > max_visible) atomicOr(a.c.err, kErrKvRange);
         if constexpr (STACK)                           // no workgroups look at the rows' own tokens
             if (!a.splits && on && a.visible[a.group_(rt * 16 * NT + t * 16 + col)] > 0) atomicOr(a.c.err, kErrKvRange);
@@ -517,7 +527,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
             far[t] = false;
             seen[t] = 0;
         }
-        const int tile0 = t0 + wave;
+        const int tile0 = t0 + member;
         if (tile0 < t1) {
             AtKeys<DP> keys;
             AtValues<DP> values;
@@ -552,19 +562,19 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
             const uint8_t* record = record_of(tile0, there ? page : 0);
             load_keys(keys, record, lane);
             if constexpr (MASK) load_mask(tile0);
-            int next = page_of(tile0 + NW);
+            int next = page_of(tile0 + TEAM);
             if constexpr (!kCareful) make_queries();
             // The next tile's keys are loaded as soon as this one's are used
             // up, its values then, and the page of the one after it.  Past
             // the end it is the last tile again, so that the loads in flight
             // are the same on every path.
-            for (int tile = tile0; tile < t1; tile += NW) {
+            for (int tile = tile0; tile < t1; tile += TEAM) {
                 load_values(values, record, lane);
                 // the loads go out before the wait for the keys
                 __builtin_amdgcn_sched_barrier(0);
                 const bool next_there = inside(next);
-                record = record_of(tile + NW, next_there ? next : 0);
-                next = page_of(tile + 2 * NW);
+                record = record_of(tile + TEAM, next_there ? next : 0);
+                next = page_of(tile + 2 * TEAM);
                 f4 s[NT][2];
 #pragma unroll
                 for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = f4{0, 0, 0, 0};
@@ -596,7 +606,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                         seen[t] |= sees[t];
                     }
                 }
-                if constexpr (MASK) load_mask(tile + NW);
+                if constexpr (MASK) load_mask(tile + TEAM);
                 all |= !edge;
                 if (edge) {
                     // past the last token that any row sees, a page holds anything
@@ -684,10 +694,10 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                 for (int r = 0; r < ND; ++r) o[t][r][e] = __builtin_nanf("");
 
     // join the waves, one tile of 16 rows after the other
-    constexpr int kPitch = DP + 4, W = DP / 8, kThreads = 64 * NW;
+    constexpr int kPitch = DP + 4, W = DP / 8;
     __shared__ __attribute__((aligned(16))) float lds[NW * 16 * kPitch];
-    __shared__ float sm[NW][16], sl[NW][16], top[16];
-    const int row0 = rt * 16 * NT, here = min(16 * NT, rows - row0);
+    __shared__ float sm[NW][16], sl[NW][16], top[TEAMS][16];
+    const int row0 = rt * 16 * NT, here = idle ? 0 : min(16 * NT, rows - row0), wave0 = team * TEAM;
     size_t part = (((size_t)(b * a.c.heads + head) * nrt + place) * splits + split) * 16 * NT;
     if constexpr (STACK)
         if (!stacked) part = a.own_part + (((size_t)(b * a.c.heads + head) * nrt + place) * splits + split) * a.own_rows;
@@ -708,33 +718,33 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                 *(f4*)&lds[(wave * 16 + col) * kPitch + ND * (4 * g + e) + r] =
                     f4{o[t][r][e], o[t][r + 1][e], o[t][r + 2][e], o[t][r + 3][e]};
         __syncthreads();
-        if (threadIdx.x < 16) {
+        if (member == 0 && lane < 16) {
             // each wave's weight, with the sum's inverse in it where the row
             // is complete
-            const int c = threadIdx.x;
-            float most = sm[0][c], sum = 0.0f, by[NW];
+            const int c = lane;
+            float most = sm[wave0][c], sum = 0.0f, by[TEAM];
 #pragma unroll
-            for (int w = 1; w < NW; ++w) most = fmaxf(most, sm[w][c]);
+            for (int w = 1; w < TEAM; ++w) most = fmaxf(most, sm[wave0 + w][c]);
 #pragma unroll
-            for (int w = 0; w < NW; ++w) {
-                by[w] = at_weight(sm[w][c], sl[w][c], most);
-                sum += by[w] * sl[w][c];
+            for (int w = 0; w < TEAM; ++w) {
+                by[w] = at_weight(sm[wave0 + w][c], sl[wave0 + w][c], most);
+                sum += by[w] * sl[wave0 + w][c];
             }
             const float scale = whole ? at_scale(most, sum) : 1.0f;
 #pragma unroll
-            for (int w = 0; w < NW; ++w) sm[w][c] = by[w] * scale;
-            top[c] = most;
-            sl[0][c] = sum;
+            for (int w = 0; w < TEAM; ++w) sm[wave0 + w][c] = by[w] * scale;
+            top[team][c] = most;
+            sl[wave0][c] = sum;
         }
         __syncthreads();
-        for (int x = threadIdx.x; x < min(16, here - t * 16) * W; x += kThreads) {
+        for (int x = member * 64 + lane; x < min(16, here - t * 16) * W; x += 64 * TEAM) {
             const int c = x / W, d = x % W * 8;
             f8 v = {};
 #pragma unroll
-            for (int w = 0; w < NW; ++w) {
+            for (int w = 0; w < TEAM; ++w) {
                 f8 y;
-                __builtin_memcpy(&y, __builtin_assume_aligned(&lds[(w * 16 + c) * kPitch + d], 16), sizeof y);
-                v += sm[w][c] * y;
+                __builtin_memcpy(&y, __builtin_assume_aligned(&lds[((wave0 + w) * 16 + c) * kPitch + d], 16), sizeof y);
+                v += sm[wave0 + w][c] * y;
             }
             if (whole) {
                 if (d < a.c.dim) write_row<T>(a, b, head, row0 + t * 16 + c, d, v);
@@ -742,7 +752,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                 const size_t at = part + t * 16 + c;
                 __builtin_memcpy(__builtin_assume_aligned(a.part_o + at * DP + d, 16), &v, sizeof v);
                 if (d == 0) {
-                    const f2 z = {top[c], sl[0][c]};
+                    const f2 z = {top[team][c], sl[wave0][c]};
                     __builtin_memcpy(__builtin_assume_aligned(a.part_ml + at * 2, 8), &z, sizeof z);
                 }
             }
@@ -979,11 +989,13 @@ constexpr int kAtFew = 5;
 
 // A window's rows read its tokens, those that the other rows of their tile are
 // ahead by under a causal order, and the first tokens.
-long long attend_window_plan(AttendRunsArgs& a, int precision) {
+static long long window_tiles(const AttendRunsArgs& a, int precision) {
     const int rows = 16 * row_tiles(a, precision), apart = (rows + a.group - 1) / a.group, ahead = (apart < a.n ? apart : a.n) - 1;
     const long long all = tiles_of(a.max_visible), some = tiles_of(a.sinks) + tiles_of((long long)a.window + ahead) + 1;
-    return split_plan(a, precision, some < all ? some : all, kAtFew);
+    return some < all ? some : all;
 }
+
+long long attend_window_plan(AttendRunsArgs& a, int precision) { return split_plan(a, precision, window_tiles(a, precision), kAtFew); }
 
 // Workgroups that read the same tokens, on one die: its cache then holds them.
 // Units of equal work, all row tiles of a sequence and head (over a shared
@@ -1080,11 +1092,23 @@ long long attend_shared_plan(AttendRunsArgs& a, int precision, AttendStack* stac
     return stack->sequences ? 0 : threads;
 }
 
+// Calls by runs whose teams are smaller than a workgroup, and not split.
+template <int DP, class T, int NT, int TEAM>
+static void launch_teams(const AttendRunsArgs& a, long long groups, hipStream_t st) {
+    constexpr int kTeams = kAtWaves<DP, T, NT> / TEAM;
+    const long long blocks = a.units_of_die ? kXcds * (((long long)a.units_of_die * a.unit_workgroups + kTeams - 1) / kTeams) : (groups + kTeams - 1) / kTeams;
+    hipLaunchKernelGGL((k_attend<DP, T, NT, kAtRuns, TEAM>), dim3((unsigned)blocks), dim3(64 * kAtWaves<DP, T, NT>), 0, st, a);
+}
+
 // The kernel of a form and, where its calls are split, the join.
 template <int DP, class T, int NT, int MODE>
 static void launch_form(const AtArgs<MODE>& a, hipStream_t st) {
     const int rows = a.n * a.group;
     long long groups = (long long)a.B * a.c.heads * ((rows + 16 * NT - 1) / (16 * NT)) * a.splits;
+    if constexpr (MODE == kAtRuns) {
+        if (a.team == 1) return launch_teams<DP, T, NT, 1>(a, groups, st);
+        if (a.team == 2) return launch_teams<DP, T, NT, 2>(a, groups, st);
+    }
     if constexpr (MODE == kAtStack) groups += a.stack_blocks;
     hipLaunchKernelGGL((k_attend<DP, T, NT, MODE>), dim3((unsigned)groups), dim3(64 * kAtWaves<DP, T, NT>), 0, st, a);
     if constexpr (MODE == kAtPlain || MODE == kAtMask) {
@@ -1121,17 +1145,48 @@ void launch_attend(const AttendArgs& a, int precision, hipStream_t st) {
     else launch<kAtPlain>(a, precision, nt, st);
 }
 
-static void launch_runs(const AttendRunsArgs& a, int precision, hipStream_t st) {
+// Waves that share a tile of rows: a workgroup's, or two or one where there are
+// rows enough to fill the chip so, since a team's start and end cost each of its
+// waves as long as three tiles take.  By an estimate in tiles of the chip's work,
+// or of one wave where that is longer (a tile takes 0.63 of the time where the
+// SIMD has no other wave), and of the end, when not all of it is busy.  us with a
+// workgroup's waves, two and one: 2 x 8191 rows with windows of 1024 and 16 first
+// (32 / 8 heads of 128, bf16) 498 / 427 / 394, 1024 such rows 38.7 / 33.7 / 39.2,
+// 19 x 278 rows of 6 / 3 fp32 heads with windows of 5 38.0 / 15.3 / 11.1, 2 x 600
+// rows of 8 / 2 heads of 256 with windows of 128 21.8 / 13.3 / 18.7, 2 x 900 fp32
+// rows of 10 / 5 heads of 64 with windows of 2000 47.2 / 55.4 / 65.6, 8 x 128 rows
+// behind 1000 tokens 38.7 / 33.6 / 39.8, 4 x 992 of 21 / 3 heads behind 6859 and 590
+// own 454 / 476 / 500.
+static int team_of(const AttendRunsArgs& a, int precision, int nt, long long tiles) {
+    const int bytes = nt * a.c.dp * (precision == WF_BF16 ? 2 : 4), waves = nt == 1 && bytes < 1024 ? 8 : 4, rows = a.n * a.group;
+    if (a.splits > 1) return waves;
+    // (as k_attend's registers allow)
+    const double slots = 4.0 * kAtTarget * (bytes <= 256 ? (nt == 1 ? 4 : 3) : (bytes <= 512 ? 2 : 1));
+    const double groups = (double)a.B * a.c.heads * ((rows + 16 * nt - 1) / (16 * nt));
+    int best = waves;
+    double least = 0.0;
+    for (int team : {waves, 2, 1}) {
+        const double one = 3.0 + (double)((tiles + team - 1) / team), all = groups * team * one / slots;
+        const double cost = (all > 0.63 * one ? all : 0.63 * one) + 0.25 * one;
+        if (team != waves && cost > 0.98 * least) continue;
+        least = cost;
+        best = team;
+    }
+    return best;
+}
+
+static void launch_runs(const AttendRunsArgs& a, int precision, long long tiles, hipStream_t st) {
     const int nt = row_tiles(a, precision), rows = a.n * a.group;
     AttendRunsArgs x = a;
+    x.team = team_of(a, precision, nt, tiles);
     deal(x, (long long)a.B * a.c.heads, (long long)((rows + 16 * nt - 1) / (16 * nt)) * a.splits);
     launch<kAtRuns>(x, precision, nt, st);
 }
 
-void launch_attend_window(const AttendRunsArgs& a, int precision, hipStream_t st) { launch_runs(a, precision, st); }
+void launch_attend_window(const AttendRunsArgs& a, int precision, hipStream_t st) { launch_runs(a, precision, window_tiles(a, precision), st); }
 
 void launch_attend_shared(const AttendRunsArgs& a, int precision, const AttendStack& stack, hipStream_t st) {
-    if (!stack.sequences) return launch_runs(a, precision, st);
+    if (!stack.sequences) return launch_runs(a, precision, tiles_of(a.max_first) + tiles_of(a.max_visible), st);
     // launches in turn, since they share the workspace
     const long long item = precision == WF_BF16 ? 2 : 4;
     for (int b = 0; b < a.B; b += stack.sequences) {

@@ -174,6 +174,7 @@ struct AttendRunsArgs : AttendArgs {
     // a prefix that lies in the cache once
     const int *first_table, *first_visible;
     int first_pages, max_first;
+    int team;                        // waves that share a tile of rows
     int window, sinks;               // window > 0: the first run is the sequence's first tokens
     // rows of all sequences together over the prefix, as workgroups before the others
     int stack_blocks, stack_splits;

@@ -109,6 +109,32 @@ def test_pages_and_values_outside_the_window(dim, n, dtype):
     c.close()
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("B,n,hq,heads,dim,L,window,sinks", [
+    (19, 130, 6, 3, 96, 140, 5, 0), (3, 333, 7, 1, 128, 400, 40, 3), (1, 2100, 8, 8, 64, 2200, 64, 1), (5, 701, 5, 5, 40, 710, 33, 33),
+    (2, 260, 16, 2, 256, 300, 20, 2), (1, 1030, 32, 8, 128, 1100, 300, 16), (9, 500, 3, 3, 64, 520, 100, 0)])
+def test_many_rows_with_short_windows(B, n, hq, heads, dim, L, window, sinks, dtype):
+    """Rows enough that a wave or two take a tile of them, the last workgroup not
+    full; causal, and unequal in no order with some that see nothing."""
+    g = np.random.default_rng(12)
+    k, v = draw((B, L, heads, dim), dtype, 1), draw((B, L, heads, dim), dtype, 2)
+    v[:, L // 2, 0, 3] = float("inf")
+    q = draw((B, n, hq, dim), dtype, 3, 0.0)
+    c, table = filled(k, v)
+    few = sorted({0, 1, n // 2, n - 2, n - 1} | set(range(0, n, 1 + n // 13)))
+    seqs = sorted({0, B // 2, B - 1})
+    for vis in (np.tile(np.arange(L - n + 1, L + 1), (B, 1)), g.integers(0, L + 1, (B, n))):
+        vis = vis.copy()
+        vis[-1, -1] = vis[0, n // 2] = 0
+        out = torch.full_like(q.cuda(), 9.0)
+        c.attend_window(q.cuda(), table, ints(vis), window, sinks, max_visible=L, out=out)
+        c.sync()
+        check(out[seqs][:, few], q[seqs][:, few], *held(k[seqs], v[seqs]), vis[seqs][:, few], dtype, windows(vis, L, window, sinks)[seqs][:, few])
+        again = c.attend_window(q.cuda(), table, ints(vis), window, sinks, max_visible=L)
+        assert torch.equal(out.nan_to_num(7.0), again.nan_to_num(7.0)) and not (out == 9).all(-1).any()
+    c.close()
+
+
 def test_a_window_that_holds_all_is_attend():
     k, v = draw((2, 500, 2, 64), "bf16", 1), draw((2, 500, 2, 64), "bf16", 2)
     q = draw((2, 3, 4, 64), "bf16", 3, 0.0).cuda()
