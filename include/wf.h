@@ -586,7 +586,8 @@ int wf_cache_attend(wf_cache_t cache, int32_t precision, const wf_rows *q, const
  *   j >= visible[b][i] - window  or  j < sinks.
  * Pages that hold none of them are not read, and their table entries need not
  * be in the pool: a caller may give them to other sequences.  The time goes by
- * window and sinks, not by the sequence.
+ * window and sinks, not by the sequence; where the rows' counts lie apart, by all
+ * that the 16 or 32 rows of a tile see together.
  *   window       positive (a row's own token counts where it is in the cache)
  *   sinks        not negative
  * The rest, the errors among it, as for wf_cache_attend without a mask.  Bits

@@ -39,8 +39,8 @@
 // each other and the join of the waves, and 1 for each tile of a wave.
 //
 // The other forms take the same tiles from other lists.  With a window a tile of
-// rows goes over its rows' first tokens and from the first token that one of them
-// sees: 64 tokens with windows of 1024 in 0 to 8192 15 us (4.1 TB/s), 1024 rows
+// rows goes over its rows' first tokens and then over the tiles that one of them
+// sees a token of: 64 tokens with windows of 1024 in 0 to 8192 15 us (4.1 TB/s), 1024 rows
 // with windows of 4096 100 (0.69 PFLOP/s).  Behind a shared prefix each row goes
 // over that and its own tokens (8 x 128 rows behind 16384 352 us, 0.78 PFLOP/s),
 // or, where sequences have few rows, those of all sequences fill the tiles over
@@ -479,6 +479,13 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     }
     const int share = splits_(tiles + splits - 1);
     const int t0 = split * share, t1 = min(tiles, t0 + share);
+    // Where the rows' counts lie apart, tiles between their windows are no row's,
+    // and are left out (a row that sees its sequence from the start may see few
+    // tokens, so its window's length says nothing).  us with and without, windows
+    // of 64: rows at 100 and 8000 tokens 6.9 / 43, at 100 and 128000 6.8 / 616; 16
+    // rows anywhere in 128000 17 / 571; rows that follow each other the same.
+    bool gaps = false;
+    if constexpr (RUNS) gaps = a.window && (low ? high - low > a.window : high > 0);
 
     b8 q[NT][NK][NQ];
     auto make_queries = [&] {
@@ -527,13 +534,29 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
             far[t] = false;
             seen[t] = 0;
         }
-        const int tile0 = t0 + member;
+        // where a tile lies in its run
+        auto place_of = [&](int tile) { return RUNS && tile >= first_tiles ? tile - first_tiles + skip : tile; };
+        // the wave's first tile from this one on that a row sees a token of
+        auto seen_from = [&](int tile) {
+            if constexpr (RUNS)
+                while (gaps && tile >= first_tiles && tile < t1) {
+                    const int at = place_of(tile) * kKvTile;
+                    int to = INT32_MAX;    // the first token from there on that a row sees
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+                        if (see[t] > at) to = min(to, max((int)from[t], at));
+                    to = __builtin_amdgcn_readfirstlane(lanes16(to, [](int x, int y) { return min(x, y); }));
+                    const int ahead = (to - at) / kKvTile;
+                    if (!ahead) break;
+                    tile += (ahead + TEAM - 1) / TEAM * TEAM;
+                }
+            return tile;
+        };
+        const int tile0 = seen_from(t0 + member);
         if (tile0 < t1) {
             AtKeys<DP> keys;
             AtValues<DP> values;
             u2 allow[NT];                  // the mask's bytes of the lane's tokens
-            // where a tile lies in its run
-            auto place_of = [&](int tile) { return RUNS && tile >= first_tiles ? tile - first_tiles + skip : tile; };
             auto page_of = [&](int tile) {
                 const int u = min(tile, t1 - 1);
                 return RUNS && u < first_tiles ? first_table[place_of(u) >> in_page] : table[place_of(u) >> in_page];
@@ -558,23 +581,25 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
             // are loaded in their place)
             auto inside = [&](int page) { return page >= 0 && page < a.c.pages; };
             const int page = tile0 >> in_page == expect ? expected : page_of(tile0);
-            bool there = inside(page), missing = !there;
+            bool there = inside(page), missing = false;
             const uint8_t* record = record_of(tile0, there ? page : 0);
             load_keys(keys, record, lane);
             if constexpr (MASK) load_mask(tile0);
-            int next = page_of(tile0 + TEAM);
+            int next_tile = seen_from(tile0 + TEAM), next = page_of(next_tile);
             if constexpr (!kCareful) make_queries();
             // The next tile's keys are loaded as soon as this one's are used
             // up, its values then, and the page of the one after it.  Past
             // the end it is the last tile again, so that the loads in flight
             // are the same on every path.
-            for (int tile = tile0; tile < t1; tile += TEAM) {
+            for (int tile = tile0; tile < t1;) {
+                missing |= !there;
                 load_values(values, record, lane);
                 // the loads go out before the wait for the keys
                 __builtin_amdgcn_sched_barrier(0);
                 const bool next_there = inside(next);
-                record = record_of(tile + TEAM, next_there ? next : 0);
-                next = page_of(tile + 2 * TEAM);
+                record = record_of(next_tile, next_there ? next : 0);
+                const int tile_after = seen_from(next_tile + TEAM);
+                next = page_of(tile_after);
                 f4 s[NT][2];
 #pragma unroll
                 for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = f4{0, 0, 0, 0};
@@ -606,7 +631,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                         seen[t] |= sees[t];
                     }
                 }
-                if constexpr (MASK) load_mask(tile + TEAM);
+                if constexpr (MASK) load_mask(next_tile);
                 all |= !edge;
                 if (edge) {
                     // past the last token that any row sees, a page holds anything
@@ -667,7 +692,8 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                 add_products<DP, NT, NP>(values.w, power, w, l, o);
                 if constexpr (kAhead) __builtin_amdgcn_s_setprio(0);
                 there = next_there;
-                missing |= !there;
+                tile = next_tile;
+                next_tile = tile_after;
             }
             if (missing && lane == 0) atomicOr(a.c.err, kErrKvPage);
         }
