@@ -1024,9 +1024,9 @@ static long long window_tiles(const AttendRunsArgs& a, int precision) {
 long long attend_window_plan(AttendRunsArgs& a, int precision) { return split_plan(a, precision, window_tiles(a, precision), kAtFew); }
 
 // Workgroups that read the same tokens, on one die: its cache then holds them.
-// Units of equal work, all row tiles of a sequence and head (over a shared
-// prefix each row tile), are dealt to the dies in the order of heads where they
-// come out even.  us with and without: 64 tokens of 32 / 8 heads of 128 behind
+// Units, all row tiles of a sequence and head (over a shared prefix each row
+// tile), are dealt to the dies in the order of heads where they come out even.
+// us with and without: 64 tokens of 32 / 8 heads of 128 behind
 // 8192 24.0 / 24.7, of 64 channels 18.5 / 19.9, 16 tokens 12.0 / 12.8, 256 tokens
 // 81.7 / 85.0.
 static void deal(AttendRunsArgs& a, long long units, long long workgroups) {
@@ -1205,7 +1205,14 @@ static void launch_runs(const AttendRunsArgs& a, int precision, long long tiles,
     const int nt = row_tiles(a, precision), rows = a.n * a.group;
     AttendRunsArgs x = a;
     x.team = team_of(a, precision, nt, tiles);
-    deal(x, (long long)a.B * a.c.heads, (long long)((rows + 16 * nt - 1) / (16 * nt)) * a.splits);
+    // Sequences may be of unequal lengths, so a die gets all of a head's or none:
+    // with fewer heads than dies one long sequence would have a die to itself.  us
+    // dealt and not, 8 sequences of 512 rows, 8 query heads a key head, windows of
+    // 4000: one of 8192 tokens and seven empty, 1 head 97 / 37, 2 heads 100 / 44, 4
+    // heads 117 / 82; all of 8192 106 / 107, 195 / 195, 376 / 378.  (Over a prefix
+    // tiles differ as their rows do, but a tile has splits for a die's compute units
+    // at least: 64 tokens of one head of which 8 see 65536 26.0 / 25.4, 8192 11.7 / 11.4.)
+    if (a.c.heads % kXcds == 0) deal(x, (long long)a.B * a.c.heads, (long long)((rows + 16 * nt - 1) / (16 * nt)) * a.splits);
     launch<kAtRuns>(x, precision, nt, st);
 }
 
