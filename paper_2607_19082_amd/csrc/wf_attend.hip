@@ -480,12 +480,13 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     const int share = splits_(tiles + splits - 1);
     const int t0 = split * share, t1 = min(tiles, t0 + share);
     // Where the rows' counts lie apart, tiles between their windows are no row's,
-    // and are left out (a row that sees its sequence from the start may see few
-    // tokens, so its window's length says nothing).  us with and without, windows
-    // of 64: rows at 100 and 8000 tokens 6.9 / 43, at 100 and 128000 6.8 / 616; 16
-    // rows anywhere in 128000 17 / 571; rows that follow each other the same.
+    // and are left out: a tile may be where one row's tokens end before it and
+    // another's begin past it (not so within a window of the first that any row
+    // sees, but a row that sees its sequence from the start may see few).  us with
+    // and without, windows of 64: rows at 100 and 8000 tokens 8.5 / 43, at 100 and
+    // 128000 8.8 / 616; 16 rows anywhere in 128000 20 / 571.
     bool gaps = false;
-    if constexpr (RUNS) gaps = a.window && (low ? high - low > a.window : high > 0);
+    if constexpr (RUNS) gaps = a.window && high - least >= kKvTile && (low == 0 || high - low > a.window);
 
     b8 q[NT][NK][NQ];
     auto make_queries = [&] {
@@ -520,9 +521,10 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
     // at a token that only other rows see, and 0 times it is not 0).  The
     // careful pass takes blocks that are not finite as zeros, and is the same
     // otherwise; a count of those that each row sees says which channels they
-    // spoil.
+    // spoil.  It is also the one that leaves out what no row sees, so that the
+    // other's loop has no part in that: with gaps, the first pass ends after a tile.
     auto pass = [&](auto careful) {
-        constexpr bool kCareful = decltype(careful)::value;
+        constexpr bool kCareful = decltype(careful)::value, kSkips = RUNS && kCareful;
         all = false;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -552,20 +554,23 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                 }
             return tile;
         };
-        const int tile0 = seen_from(t0 + member);
+        const int tile0 = seen_from(t0 + member), end = gaps && !kCareful ? min(t1, tile0 + 1) : t1;
         if (tile0 < t1) {
             AtKeys<DP> keys;
             AtValues<DP> values;
             u2 allow[NT];                  // the mask's bytes of the lane's tokens
+            // past the end the last tile again, or the first where the last may be no row's
+            auto of_list = [&](int tile) { return kSkips && tile >= t1 ? tile0 : min(tile, end - 1); };
+            auto further = [&](int tile) { return kSkips ? seen_from(tile) : tile; };
             auto page_of = [&](int tile) {
-                const int u = min(tile, t1 - 1);
+                const int u = of_list(tile);
                 return RUNS && u < first_tiles ? first_table[place_of(u) >> in_page] : table[place_of(u) >> in_page];
             };
             auto record_of = [&](int tile, int page) {
-                return pool + (size_t)page * page_bytes + (size_t)(place_of(min(tile, t1 - 1)) & ((1 << in_page) - 1)) * L::kRecord;
+                return pool + (size_t)page * page_bytes + (size_t)(place_of(of_list(tile)) & ((1 << in_page) - 1)) * L::kRecord;
             };
             auto load_mask = [&](int tile) {
-                const int at = min(tile, t1 - 1) * kKvTile + 8 * g;
+                const int at = of_list(tile) * kKvTile + 8 * g;
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     if (at + 8 <= a.max_visible) {
@@ -581,25 +586,24 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
             // are loaded in their place)
             auto inside = [&](int page) { return page >= 0 && page < a.c.pages; };
             const int page = tile0 >> in_page == expect ? expected : page_of(tile0);
-            bool there = inside(page), missing = false;
+            bool there = inside(page), missing = !there;
             const uint8_t* record = record_of(tile0, there ? page : 0);
             load_keys(keys, record, lane);
             if constexpr (MASK) load_mask(tile0);
-            int next_tile = seen_from(tile0 + TEAM), next = page_of(next_tile);
+            // the wave's next tile and the one after it, where they may be further on
+            int second = further(tile0 + TEAM), third = further(second + TEAM), next = page_of(second);
             if constexpr (!kCareful) make_queries();
             // The next tile's keys are loaded as soon as this one's are used
             // up, its values then, and the page of the one after it.  Past
-            // the end it is the last tile again, so that the loads in flight
-            // are the same on every path.
-            for (int tile = tile0; tile < t1;) {
-                missing |= !there;
+            // the end it is another again, so that the loads in flight are the
+            // same on every path.
+            for (int tile = tile0; tile < end; tile = kSkips ? second : tile + TEAM, second = third, third = further(second + TEAM)) {
                 load_values(values, record, lane);
                 // the loads go out before the wait for the keys
                 __builtin_amdgcn_sched_barrier(0);
                 const bool next_there = inside(next);
-                record = record_of(next_tile, next_there ? next : 0);
-                const int tile_after = seen_from(next_tile + TEAM);
-                next = page_of(tile_after);
+                record = record_of(kSkips ? second : tile + TEAM, next_there ? next : 0);
+                next = page_of(kSkips ? third : tile + 2 * TEAM);
                 f4 s[NT][2];
 #pragma unroll
                 for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = f4{0, 0, 0, 0};
@@ -631,7 +635,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                         seen[t] |= sees[t];
                     }
                 }
-                if constexpr (MASK) load_mask(next_tile);
+                if constexpr (MASK) load_mask(tile + TEAM);
                 all |= !edge;
                 if (edge) {
                     // past the last token that any row sees, a page holds anything
@@ -692,8 +696,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                 add_products<DP, NT, NP>(values.w, power, w, l, o);
                 if constexpr (kAhead) __builtin_amdgcn_s_setprio(0);
                 there = next_there;
-                tile = next_tile;
-                next_tile = tile_after;
+                missing |= !there;
             }
             if (missing && lane == 0) atomicOr(a.c.err, kErrKvPage);
         }
@@ -707,7 +710,7 @@ __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, 
                 for (int r = 0; r < ND; ++r)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) nan |= o[t][r][e] != o[t][r][e];
-            return !__any(nan);
+            return !gaps && !__any(nan);
         }
     };
     if (!pass(std::false_type())) pass(std::true_type());
