@@ -499,6 +499,19 @@ class _TokenCalls:
         raise ValueError(f"{name}: expected a {dtype} tensor {tuple(shape)} on device {self._device} with contiguous "
                          f"channels, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
 
+    def _output(self, t, shape, dtype, name):
+        """The rows of a tensor that a caller gives to be written.  Autograd does not
+        see the write: a tensor that it follows would keep the gradient of what it
+        held before."""
+        rows = self._rows(t, shape, dtype, name)
+        if t.requires_grad:
+            import torch
+            if torch.is_grad_enabled():
+                raise ValueError(f"{name}: requires a gradient, which these calls do not give; give a tensor that does not, "
+                                 "or call under torch.no_grad()")
+            torch.autograd.graph.increment_version(t)
+        return rows
+
     def _ints(self, t, shape, name):
         if t.dtype is self._int and t.shape == shape and t.get_device() == self._device and t.is_contiguous():
             return t.data_ptr()
@@ -613,7 +626,7 @@ class Cache(_TokenCalls):
             k, v = out
             dtype = k.dtype
             precision = self._type(dtype)
-            k_rows, v_rows = self._rows(k, shape, dtype, "k"), self._rows(v, shape, dtype, "v")
+            k_rows, v_rows = self._output(k, shape, dtype, "k"), self._output(v, shape, dtype, "v")
         rc = self._lib.wf_cache_read(
             self._h, precision, k_rows, v_rows, B, n, p_table, pages, self._ints(first, (B,), "first"),
             None if counts is None else self._ints(counts, (B,), "counts"), self._stream(stream, k, v, table, first, counts))
@@ -628,7 +641,8 @@ class Cache(_TokenCalls):
         it allows; a row that sees none gives zeros.  q_heads is a multiple of
         the cache's heads; scale defaults to dim ** -0.5.  max_visible bounds
         visible (default: the mask's width, or all that the table holds; a
-        tighter bound makes a better launch).  Outputs carry no gradient."""
+        tighter bound makes a better launch).  Outputs carry no gradient; an `out`
+        that requires one is refused where gradients are recorded."""
         shape, dtype = q.shape, q.dtype
         if len(shape) != 4:
             raise ValueError(f"q: expected four dimensions, got {tuple(shape)}")
@@ -643,7 +657,7 @@ class Cache(_TokenCalls):
         if out is None:
             out, out_rows = self._new(shape, dtype, stream, like=q if q.is_contiguous() else None)
         else:
-            out_rows = self._rows(out, shape, dtype, "out")
+            out_rows = self._output(out, shape, dtype, "out")
         p_mask = strides = None
         if mask is not None:
             if mask.get_device() != self._device or mask.dtype != self._bool or mask.shape != (B, n, max_visible) or \
@@ -677,7 +691,7 @@ class Cache(_TokenCalls):
         if out is None:
             out, out_rows = self._new(shape, dtype, stream, like=q if q.is_contiguous() else None)
         else:
-            out_rows = self._rows(out, shape, dtype, "out")
+            out_rows = self._output(out, shape, dtype, "out")
         return B, n, hq, precision, q_rows, out, out_rows, p_table, pages, max_visible
 
     def attend_window(self, q, table, visible, window, sinks=0, scale=None, max_visible=None, out=None, stream=None):
@@ -777,7 +791,8 @@ class HeadNorm(_TokenCalls):
         [B][n], with two axes [B][n][2] (None where nothing is rotated); gains are
         fp32 [dim] (None: ones).  With counts (int32 [B]) tokens from counts[b] on
         are left as they were in `out` (a new tensor holds anything there).
-        Outputs carry no gradient."""
+        Outputs carry no gradient; an `out` that requires one is refused where
+        gradients are recorded."""
         shape, dtype = q.shape, q.dtype
         if len(shape) != 4:
             raise ValueError(f"q: expected four dimensions, got {tuple(shape)}")
@@ -802,9 +817,9 @@ class HeadNorm(_TokenCalls):
                 ko, ko_rows = self._new(k_shape, dtype, stream, like=k if k.is_contiguous() else None)
         else:
             qo, ko = (out, None) if k is None else out
-            qo_rows = self._rows(qo, q_shape, dtype, "out")
+            qo_rows = self._output(qo, q_shape, dtype, "out")
             if k is not None:
-                ko_rows = self._rows(ko, k_shape, dtype, "out")
+                ko_rows = self._output(ko, k_shape, dtype, "out")
         p_positions = None
         if self.rotated and positions is None:
             raise ValueError("positions: needed where channels are rotated")
