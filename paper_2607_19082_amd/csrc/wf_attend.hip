@@ -44,8 +44,8 @@
 // with windows of 4096 100 (0.69 PFLOP/s).  Behind a shared prefix each row goes
 // over that and its own tokens (8 x 128 rows behind 16384 352 us, 0.78 PFLOP/s),
 // or, where sequences have few rows, those of all sequences fill the tiles over
-// the prefix together: 64 tokens behind 8192, 32 / 8 heads, 24 us, where 64 times
-// the prefix takes 68.
+// the prefix together: 64 tokens behind 8192, with 100 of their own each, 32 / 8
+// heads, 24 us, where 64 times the prefix takes 68.
 #include <cmath>
 #include <type_traits>
 
@@ -332,9 +332,10 @@ template <int DP, class T, int NT, int MODE, int TEAM = kAtWaves<DP, T, NT>>
 __global__ __launch_bounds__((64 * kAtWaves<DP, T, NT>), (kAtWavesOfSimd<DP, T, NT>)) void k_attend(AtArgs<MODE> a) {
     constexpr bool MASK = MODE == kAtMask, RUNS = MODE == kAtRuns, STACK = MODE == kAtStack;
     // A wave at its values' products goes ahead of the SIMD's others.  us without
-    // and with: 8 x 128 rows behind 16384 (8 heads of 128, bf16) 371 / 366, 4 x 128
-    // behind 8192 in fp32 184 / 178, 64 tokens behind 8192 in bf16 32.9 / 32.1, in
-    // fp32 36.8 / 35.7; of 64 channels in fp32, two tiles of rows, 58.2 / 60.6.
+    // and with, 32 / 8 heads of 128: 8 x 128 causal rows behind 16384 in bf16 360 /
+    // 357, 4 x 128 behind 8192 in fp32 180 / 173, 64 tokens behind 8192 with 777 of
+    // their own each in bf16 34.5 / 34.2, in fp32 46.5 / 44.8; of 64 channels in
+    // fp32, two tiles of rows, 58.2 / 60.6.
     constexpr bool kAhead = (RUNS || STACK) && !(NT == 2 && sizeof(T) == 4);
     constexpr int NW = kAtWaves<DP, T, NT>, NQ = AtParts<T>::kQ, NP = AtParts<T>::kP, NK = DP / 32, ND = DP / 16;
     constexpr int TEAMS = NW / TEAM;
@@ -1029,9 +1030,10 @@ long long attend_window_plan(AttendRunsArgs& a, int precision) { return split_pl
 // Workgroups that read the same tokens, on one die: its cache then holds them.
 // Units, all row tiles of a sequence and head (over a shared prefix each row
 // tile), are dealt to the dies in the order of heads where they come out even.
-// us with and without: 64 tokens of 32 / 8 heads of 128 behind
-// 8192 24.0 / 24.7, of 64 channels 18.5 / 19.9, 16 tokens 12.0 / 12.8, 256 tokens
-// 81.7 / 85.0.
+// us with and without: 64 tokens of 32 / 8 heads of 128 behind 8192, 100 of their
+// own each, 24.1 / 25.0, 16 such tokens 12.6 / 13.1; without own tokens 64 of 64
+// channels 19.6 / 20.2, 256 of 128 65.0 / 66.2; 8 x 128 causal rows behind 16384
+// 357 / 372.
 static void deal(AttendRunsArgs& a, long long units, long long workgroups) {
     a.units_of_die = 0;
     if (units % kXcds) return;
